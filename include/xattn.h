@@ -138,11 +138,37 @@ int xattn_mla_decode(const void* q, const void* const* c_ptrs, const int32_t* kv
                      int n_heads, int d_latent, int d_rope, float scale, void* out, float* lse, void* stream);
 
 /*
+ * Attention of whole prompts: the new tokens of a batch of sequences of different lengths, packed one behind the other, against
+ * the sequences' keys (the same operator of section 4.3 "Operator Adaptation" in the step that fills the cache: ranges instead of a
+ * block table).  A prompt may come in chunks (a cached prefix in front of its new tokens), and decoding sequences with one new
+ * token may be among them.  Sequence b has the packed rows [q_starts[b], q_starts[b + 1]), its q_len of them, and its new token
+ * t sees Lv = kv_lens[b] - q_len + t + 1 keys; s_j, out and lse as for xattn_decode, with row q_starts[b] + t for [b, t].
+ * q        DEVICE  bf16 [total_q, n_q_heads, head_dim], contiguous, 16-byte aligned
+ * k_ptrs, v_ptrs   as for xattn_decode; rows at or past kv_lens[b] are never read, and a sequence's K may exceed 4 GiB
+ * q_starts DEVICE  int32[batch + 1], ascending from 0; q_starts[batch] <= total_q.  Sequences without new tokens may be among
+ *                  them.  Rows of out and lse from q_starts[batch] on are left as they were.  Bounds that do not ascend, or pass total_q, are
+ *                  cut to it and leave rows unspecified, but nothing outside the buffers is touched.
+ * kv_lens  DEVICE  int32[batch]; keys visible to the sequence's last new token (its K/V are already written).  Tokens without
+ *                  visible keys (kv_len < q_len) get out = 0 and lse = -inf.
+ * batch 1..4096; total_q 1..2^24, the rows that q, out and lse have; total_q * n_q_heads <= 2^30; head_dim 128; n_q_heads <=
+ * 1024, a multiple of n_kv_heads.  Otherwise XATTN_EUNSUPPORTED.  scale finite.
+ * out      DEVICE  bf16 [total_q, n_q_heads, head_dim], 16-byte aligned, not overlapping the inputs;  lse DEVICE fp32 [total_q, n_q_heads] or NULL
+ * Same stream, capture and ownership rules as xattn_decode, same workspace (of at least xattn_prefill_workspace_bytes).
+ * Numerics: scores, maxima and sums in fp32; a softmax weight enters the value product as one bf16 (off by 2^-8 of it at most,
+ * xattn_decode keeps 24 bits), the result is rounded to bf16 once.  q and the keys and values of a sequence must be finite: an
+ * infinity or NaN leaves the sequence's rows unspecified, and no others.
+ */
+int xattn_prefill(const void* q, const void* const* k_ptrs, const void* const* v_ptrs, const int32_t* q_starts,
+                  const int32_t* kv_lens, int batch, int total_q, int n_q_heads, int n_kv_heads, int head_dim, float scale,
+                  void* out, float* lse, void* stream);
+
+/*
  * Workspace for the partial results of split sequences (section 4.4.3: the parts of a split
  * sequence are computed by different compute units and aggregated afterwards).
  * xattn_workspace_bytes:     upper bound on the bytes one xattn_decode call of this shape uses
  *                            (0 and a message for an unsupported shape).
  * xattn_mla_workspace_bytes: the same for one xattn_mla_decode call.
+ * xattn_prefill_workspace_bytes: the same for one xattn_prefill call, which takes no less than that.
  * xattn_set_workspace:       hand the library a DEVICE buffer (256-byte aligned) for the current
  *                            device, used by calls on every stream; the caller keeps ownership and
  *                            keeps it alive while calls are in flight or graphs that recorded them
@@ -160,6 +186,7 @@ int xattn_mla_decode(const void* q, const void* const* c_ptrs, const int32_t* kv
  */
 size_t xattn_workspace_bytes(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim);
 size_t xattn_mla_workspace_bytes(int batch, int q_len, int n_heads, int d_latent, int d_rope);
+size_t xattn_prefill_workspace_bytes(int batch, int total_q, int n_q_heads, int n_kv_heads, int head_dim);
 int xattn_set_workspace(void* dev_ptr, size_t bytes);
 
 /*
@@ -326,6 +353,34 @@ int xtensor_range_pages(void* range, int64_t* page_ids_out, int n);
 int xattn_write_kvcache(const void* k_new, const void* v_new, void* const* k_ptrs, void* const* v_ptrs,
                         const int32_t* kv_lens, int batch, int q_len, int n_kv_heads, int head_dim,
                         void* stream);
+
+/*
+ * Rotary positions and append in one: turns the heads of the packed new rows of q and k_new by their positions, writes q's to
+ * q_out (what xattn_prefill or xattn_decode takes next) and k's, with v_new as it is, to the sequences' ranges, where
+ * xattn_write_kvcache would put them: row q_starts[b] + t of the batch is row kv_lens[b] - q_len + t of sequence b (kv_lens: the
+ * lengths AFTER the append; a row whose index would be negative is not written, its q is turned all the same).
+ * Rotation: with F = sum of sections[], the first 2 F values of a head are F pairs, the rest is left as it is.  Pair i is the
+ * values (i, F + i), or with XATTN_ROPE_PAIRS (2 i, 2 i + 1), and is turned by the angle pos[axis of i][row] * inv_freq[i]:
+ *     (x, y) -> (x cos - y sin, y cos + x sin)
+ * Axes (one for text; time, height, width for images and video): axis a has sections[a] frequencies, one axis behind the
+ * other, or with XATTN_ROPE_DEALT dealt out in turn, passing over an axis that has all of its own.
+ * q, k_new, v_new  DEVICE bf16, rows of n_q_heads (n_kv_heads) * head_dim values, q_stride (k_stride, v_stride) values apart, so that
+ *                  the three may be columns of one projection's output; addresses and strides multiples of 16 bytes
+ * pos       DEVICE int32 [n_axes, total_q], any sign; inv_freq DEVICE fp32 [F], in radians per position (scaled ones included);
+ *           NULL only where F is 0, which splits and appends without turning.
+ *           The angle is reduced in double precision.
+ * sections  HOST int32[n_axes], n_axes 1..4; F a multiple of 8, at most head_dim / 2
+ * k_ptrs, v_ptrs, q_starts, kv_lens  DEVICE, as for xattn_prefill (the ranges are written here; the rows must be backed)
+ * q_out     DEVICE bf16 [total_q, n_q_heads, head_dim], 16-byte aligned; may be q itself where q_stride is n_q_heads * head_dim, and
+ *           overlaps no input otherwise.  Rows of it from q_starts[batch] on are left as they were.
+ * batch 1..4096, total_q 1..2^24, total_q * n_q_heads <= 2^30, heads up to 1024 each, head_dim a multiple of 16 up to 256
+ * Asynchronous on `stream`, no workspace; may be captured.  Two rows must not go to the same row of a range.
+ */
+enum { XATTN_ROPE_PAIRS = 1, XATTN_ROPE_DEALT = 2 };
+int xattn_rope_kvcache(const void* q, const void* k_new, const void* v_new, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                       const int32_t* pos, const float* inv_freq, const int32_t* sections, int n_axes, int flags,
+                       void* const* k_ptrs, void* const* v_ptrs, const int32_t* q_starts, const int32_t* kv_lens, int batch,
+                       int total_q, int n_q_heads, int n_kv_heads, int head_dim, void* q_out, void* stream);
 
 /* Synchronous copies between HOST memory and any DEVICE address (mapped ranges included). */
 int xtensor_upload(void* dst_device, const void* src_host, size_t bytes);

@@ -7,5 +7,7 @@ from .binding import (XTENSOR_PAGE_ALLOCATED, XTENSOR_PAGE_FREE, XTENSOR_PAGE_MA
                       xattn_mla_decode, xattn_mla_workspace_bytes, xattn_write_kvcache, xtensor_close, xtensor_grow, xtensor_open, xtensor_page_info,
                       xtensor_pool_counts, xtensor_pool_create, xtensor_pool_destroy, xtensor_premap_async,
                       xtensor_premap_wait, xtensor_range_pages)
-from .binding import XBEAM_CHECK_INPUT, XBEAM_FULL_SORT, xbeam_select  # noqa: F401
+from .binding import (XATTN_ROPE_DEALT, XATTN_ROPE_PAIRS, XBEAM_BF16, XBEAM_CHECK_INPUT, XBEAM_FP16, XBEAM_FP32, XBEAM_FULL_SORT,  # noqa: F401
+                      xattn_prefill, xattn_prefill_workspace_bytes, xattn_rope_kvcache, xbeam_logprobs, xbeam_logprobs_workspace_bytes,
+                      xbeam_select)
 from .kvstore import KVStore  # noqa: F401

@@ -24,8 +24,11 @@ EXPORTS = ["xattn_last_error", "xattn_decode", "xattn_decode_noalloc", "xattn_wo
            "xtensor_physical_view", "xtensor_upload", "xtensor_download",
            "xtensor_pool_create", "xtensor_pool_destroy", "xtensor_pool_counts", "xtensor_page_info",
            "xtensor_open", "xtensor_grow", "xtensor_premap_async", "xtensor_premap_wait", "xtensor_close",
-           "xtensor_range_pages", "xattn_write_kvcache", "xattn_mla_decode", "xattn_mla_workspace_bytes", "xbeam_select"]
+           "xtensor_range_pages", "xattn_write_kvcache", "xattn_mla_decode", "xattn_mla_workspace_bytes", "xbeam_select",
+           "xattn_prefill", "xattn_prefill_workspace_bytes", "xattn_rope_kvcache", "xbeam_logprobs", "xbeam_logprobs_workspace_bytes"]
 XBEAM_FULL_SORT, XBEAM_CHECK_INPUT = 1, 2
+XBEAM_BF16, XBEAM_FP16, XBEAM_FP32 = 0, 1, 2
+XATTN_ROPE_PAIRS, XATTN_ROPE_DEALT = 1, 2
 XTENSOR_PAGE_FREE, XTENSOR_PAGE_ALLOCATED, XTENSOR_PAGE_MAPPED, XTENSOR_PAGE_REUSABLE = 0, 1, 2, 3
 
 
@@ -39,7 +42,7 @@ _lib = None
 
 
 def _signatures():
-    vp, i32, sz, u64, f32 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint64, ctypes.c_float
+    vp, i32, sz, u64, f32, i64 = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_uint64, ctypes.c_float, ctypes.c_int64
     P = ctypes.POINTER
     return {
         "xattn_last_error": (ctypes.c_char_p, []),
@@ -69,6 +72,11 @@ def _signatures():
         "xattn_mla_decode": (i32, [vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp]),
         "xbeam_select": (i32, [vp, vp, vp, i32, i32, i32, i32, vp, vp, vp, vp]),
         "xattn_write_kvcache": (i32, [vp, vp, vp, vp, vp, i32, i32, i32, i32, vp]),
+        "xattn_prefill": (i32, [vp, vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp]),
+        "xattn_prefill_workspace_bytes": (sz, [i32] * 5),
+        "xattn_rope_kvcache": (i32, [vp, vp, vp, i64, i64, i64, vp, vp, P(i32), i32, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]),
+        "xbeam_logprobs": (i32, [vp, i32, i64, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp, vp]),
+        "xbeam_logprobs_workspace_bytes": (sz, [i32] * 3),
     }
 
 
@@ -296,6 +304,60 @@ def xattn_mla_decode(q, c_ptrs, kv_lens, batch: int, q_len: int, n_heads: int, d
                                                        scale if type(scale) is float else ctypes.c_float(scale), _ptr(out), _ptr(lse), stream)
     if status < 0:
         _check(status)
+
+
+def xattn_prefill(q, k_ptrs, v_ptrs, q_starts, kv_lens, batch: int, total_q: int, n_q_heads: int, n_kv_heads: int, head_dim: int,
+                  scale: float, out, lse=None, stream=None) -> None:
+    """Enqueue attention of the packed new tokens of a batch of prompts; see include/xattn.h."""
+    if stream is not None and not isinstance(stream, int):
+        stream = int(stream.cuda_stream)
+    status = (_lib or load_library()).xattn_prefill(_ptr(q), _ptr(k_ptrs), _ptr(v_ptrs), _ptr(q_starts), _ptr(kv_lens), batch, total_q, n_q_heads,
+                                                    n_kv_heads, head_dim, scale if type(scale) is float else ctypes.c_float(scale),
+                                                    _ptr(out), _ptr(lse), stream)
+    if status < 0:
+        _check(status)
+
+
+def xattn_prefill_workspace_bytes(batch: int, total_q: int, n_q_heads: int, n_kv_heads: int, head_dim: int = 128) -> int:
+    n = int(load_library().xattn_prefill_workspace_bytes(batch, total_q, n_q_heads, n_kv_heads, head_dim))
+    if n == 0:
+        raise XattnError(XATTN_EUNSUPPORTED, xattn_last_error())
+    return n
+
+
+def xattn_rope_kvcache(q, k_new, v_new, q_stride: int, k_stride: int, v_stride: int, pos, inv_freq, sections, flags: int, k_ptrs, v_ptrs,
+                       q_starts, kv_lens, batch: int, total_q: int, n_q_heads: int, n_kv_heads: int, head_dim: int, q_out, stream=None) -> None:
+    """Enqueue the rotation of q and k_new and the append of k_new and v_new; see include/xattn.h.  Strides in values; sections: a
+    sequence of integers, one per axis."""
+    if stream is not None and not isinstance(stream, int):
+        stream = int(stream.cuda_stream)
+    n_axes = len(sections)
+    status = (_lib or load_library()).xattn_rope_kvcache(_ptr(q), _ptr(k_new), _ptr(v_new), q_stride, k_stride, v_stride, _ptr(pos), _ptr(inv_freq),
+                                                         (ctypes.c_int * n_axes)(*sections), n_axes, flags, _ptr(k_ptrs), _ptr(v_ptrs),
+                                                         _ptr(q_starts), _ptr(kv_lens), batch, total_q, n_q_heads, n_kv_heads, head_dim,
+                                                         _ptr(q_out), stream)
+    if status < 0:
+        _check(status)
+
+
+def xbeam_logprobs(logits, dtype: int, row_stride: int, rows: int, vocab: int, scale: float, tokens=None, top_k: int = 0, token_lp=None,
+                   top_lp=None, top_tok=None, lse=None, entropy=None, stream=None) -> None:
+    """Enqueue log-probabilities, top alternatives and entropy of rows of logits; see include/xbeam.h.  All pointers are device
+    addresses; row_stride in values."""
+    if stream is not None and not isinstance(stream, int):
+        stream = int(stream.cuda_stream)
+    status = (_lib or load_library()).xbeam_logprobs(_ptr(logits), dtype, row_stride, rows, vocab,
+                                                     scale if type(scale) is float else ctypes.c_float(scale), _ptr(tokens), top_k,
+                                                     _ptr(token_lp), _ptr(top_lp), _ptr(top_tok), _ptr(lse), _ptr(entropy), stream)
+    if status < 0:
+        _check(status)
+
+
+def xbeam_logprobs_workspace_bytes(rows: int, vocab: int, top_k: int) -> int:
+    n = int(load_library().xbeam_logprobs_workspace_bytes(rows, vocab, top_k))
+    if n == 0:
+        raise XattnError(XATTN_EUNSUPPORTED, xattn_last_error())
+    return n
 
 
 def xbeam_select(beam_lp, cand_lp, cand_tok=None, flags: int = 0, out_lp=None, out_parent=None, out_tok=None,

@@ -247,6 +247,17 @@ int timing_events(hipEvent_t** events_out) {
 
 }  // namespace
 
+int with_workspace(const char* who, size_t bytes, void* stream, WorkspaceLaunchFn launch, void* context) {
+    std::lock_guard<std::mutex> lock(g_mutex);
+    DeviceState* d = nullptr;
+    int st = device_state(&d, nullptr);
+    if (st != XATTN_OK) return st;
+    char* ws = nullptr;
+    size_t have = 0;
+    st = acquire_workspace(d, bytes, static_cast<hipStream_t>(stream), who, &ws, &have);
+    return st != XATTN_OK ? st : launch(context, ws);
+}
+
 // xattn_decode and its variants: argument checks, workspace, launch.  `fixed_workspace`, when given,
 // supplies the workspace instead of the per-stream one (and the call is never timed: events allocate).
 int decode_call(const char* who, FixedWorkspaceFn fixed_workspace, const void* q, const void* const* k_ptrs,
