@@ -5,14 +5,17 @@
 // Bound by memory: a row is read once.  Every lane keeps m (its own maximum), s and t of its values, moved on when m moves, and the
 // lanes' are put together at the end.
 //
-// Alternatives: a lane's maximum is there anyway, and if in each of the 8 waves ceil(k / 8) lanes have a maximum of tau or
-// more, so have k values of the row: what is below tau is none of the k.  So values are only compared with tau, eight at
-// a time, by their maximum; those that pass go to the wave's list in LDS, with their index.  tau rises as the row is read, and of
-// random rows a few times k values pass.  A list that is full (a row that ascends, or whose values are all equal) is cut to its k
-// best.  Order everywhere: value descending, then index ascending, as one 64-bit number.
+// Alternatives: a lane's maximum is there anyway, and if in each of some waves ceil(k / 8) lanes have a maximum of tau or more, and
+// those are k in all, so have k values of the row: what is below tau is none of the k.  So of every chunk of 16 bytes only the maximum
+// is compared with tau; a chunk that passes goes to its wave's list in LDS, by (maximum, place).  tau rises as the row is read, and
+// of random rows a few times k chunks pass.  A list that is full (a row that ascends, or whose values are all equal) is cut to its k best
+// chunks.  The k best values are in the k best chunks: a chunk behind k others has k values ahead of all of its own.  These are read
+// again at the end, and their values put into order.  Order everywhere: value descending, then index ascending, as one 64-bit number.
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "../../include/xbeam.h"
 #include "xattn_device.h"
@@ -22,12 +25,15 @@
 namespace xattn {
 namespace {
 
-constexpr int kRowWaves = 8;
-constexpr int kRowThreads = 64 * kRowWaves;
-constexpr int kVec = 8;                          // values per lane and load
-constexpr int kStep = 64 * kVec;                 // values per wave and load
-constexpr int kLoads = 2;                        // loads of a wave in a row
-constexpr int kLeastPart = kRowWaves * kStep;    // values
+constexpr int kRowWaves = 8;                     // waves of a workgroup; kFewWaves where rows are short
+constexpr int kFewWaves = 2;
+constexpr int kStep = 512;                       // values that a wave loads as one row of 8 (or two of 4) per lane
+constexpr int kLoads = 2;                        // steps of a wave in a round
+constexpr int kVals = kLoads * kStep / 64;       // a lane's values in a round
+constexpr int kAtOnceSize = kRowWaves * kLoads * kStep;      // values that a workgroup's registers hold
+constexpr int kAtOnce = -1;
+constexpr int kParts = 256;                      // workgroups that rows are cut for
+constexpr int kFewRounds = 6;                    // of a row that is not cut
 constexpr int kMostMerged = 8192;                // candidates that the merge of a row's parts holds
 constexpr float kFar = 1e30f;                    // logits beyond are summed up in a second pass, whose differences do not overflow
 
@@ -48,30 +54,21 @@ __device__ __forceinline__ float to_float(Bf16 x) { return __uint_as_float((uint
 __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_float(float x) { return x; }
 
-// Eight values as they lie in memory; rows begin where they like.
-template <typename T> struct Raw;
-typedef uint32_t u32x4_un __attribute__((ext_vector_type(4), aligned(2)));
-template <> struct Raw<Bf16> {
+// Sixteen bytes of a row, which may begin anywhere.
+typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
+template <typename T> struct Chunk {
+    static constexpr int kCount = 16 / (int)sizeof(T);
     u32x4_t x;
-    __device__ __forceinline__ void load(const Bf16* p) { x = *reinterpret_cast<const u32x4_un*>(p); }
-    __device__ __forceinline__ float get(int i) const { return i & 1 ? bf16_hi(x[i >> 1]) : bf16_lo(x[i >> 1]); }
-};
-template <> struct Raw<__half> {
-    u32x4_t x;
-    __device__ __forceinline__ void load(const __half* p) { x = *reinterpret_cast<const u32x4_un*>(p); }
+    __device__ __forceinline__ void load(const T* p) {
+        using words = typename std::conditional<sizeof(T) == 4, words_at_4, words_at_2>::type;
+        x = __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
+    }
     __device__ __forceinline__ float get(int i) const {
-        const uint32_t w = x[i >> 1];
-        return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? w >> 16 : w));
+        if constexpr (sizeof(T) == 4) return __uint_as_float(x[i]);
+        else if constexpr (std::is_same<T, Bf16>::value) return i & 1 ? bf16_hi(x[i >> 1]) : bf16_lo(x[i >> 1]);
+        else return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? x[i >> 1] >> 16 : x[i >> 1]));
     }
-};
-typedef uint32_t u32x4_un4 __attribute__((ext_vector_type(4), aligned(4)));
-template <> struct Raw<float> {
-    u32x4_t x[2];
-    __device__ __forceinline__ void load(const float* p) {
-        x[0] = *reinterpret_cast<const u32x4_un4*>(p);
-        x[1] = *reinterpret_cast<const u32x4_un4*>(p + 4);
-    }
-    __device__ __forceinline__ float get(int i) const { return __uint_as_float(x[i >> 2][i & 3]); }
 };
 
 // m, s and t of some values; m is finite.
@@ -88,6 +85,11 @@ __device__ __forceinline__ void add(Sums& a, float y) {      // y = (x - m) * c
     const float e = fast_exp2(y);
     a.s += e;
     a.t = __builtin_fmaf(e, fmaxf(y, -1000.0f), a.t);        // e is 0 from -150 on, and -inf times that no number
+}
+
+// How many of the lanes in `lanes` are below this one.
+__device__ __forceinline__ int before(unsigned long long lanes) {
+    return (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(lanes >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)lanes, 0u));
 }
 
 // The k best of the `count` candidates of a wave's list, which it leaves at the list's start; returns the least of them.
@@ -110,15 +112,25 @@ __device__ __forceinline__ uint64_t cut_list(uint64_t* list, int count, int k, i
 #pragma unroll
     for (int i = 0; i < kCap / 64; ++i) {
         const unsigned long long keep = __ballot(c[i] >= least);
-        if (c[i] >= least) list[at + __builtin_popcountll(keep & ((1ull << lane) - 1))] = c[i];
+        if (c[i] >= least) list[at + before(keep)] = c[i];
         at += __builtin_popcountll(keep);
     }
     __builtin_amdgcn_wave_barrier();
     return least;
 }
 
-// The r-th largest of the lanes' keys, or a little less (16 bits of it).
-__device__ __forceinline__ uint32_t nth_key(uint32_t key, int r) {
+// The key of the r-th largest of the lanes' values, or a little less (16 bits of it).
+__device__ __forceinline__ uint32_t nth_key(float x, int r) {
+    if (r <= 4) {      // a few times the largest of those left; lanes that share it count together
+        float best = wave_max(x);
+        for (int left = r - __builtin_popcountll(__ballot(x == best)); left > 0; left -= __builtin_popcountll(__ballot(x == best))) {
+            x = x == best ? kNegInf : x;
+            if (__ballot(x > kNegInf) == 0) return 0u;
+            best = wave_max(x);
+        }
+        return order_key(best);
+    }
+    const uint32_t key = order_key(x);
     uint32_t at = 0;
 #pragma unroll
     for (int bit = 31; bit >= 16; --bit) {
@@ -128,59 +140,223 @@ __device__ __forceinline__ uint32_t nth_key(uint32_t key, int r) {
     return at;
 }
 
-// Puts n candidates (at most `room`, a power of two) of the workgroup into order.  Called by all threads; LDS is ready before and after.
-template <int kThreads>
-__device__ __forceinline__ void sort_candidates(uint64_t* list, int n, int room, int tid) {
-    if (n <= 128) {
-        const uint64_t mine = tid < n ? list[tid] : 0;
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += list[j] > mine;
-        __syncthreads();
-        if (tid < n) list[rank] = mine;
-        __syncthreads();
-        return;
-    }
-    int size = 256;
-    while (size < n) size <<= 1;
-    if (size > room) size = room;
-    for (int i = n + tid; i < size; i += kThreads) list[i] = 0;
+// What the workgroup's threads need of LDS to pick and order candidates.
+struct PickSpace {
+    uint32_t bins[3][256];       // one counts, one is clear for the next round, one may still be read
+    int counts[kRowWaves];
+    uint64_t list[kMaxTopK + 8];
+};
+
+// Leaves the k best of the threads' candidates (more than k of them; 0: none) and zeroes the others: their keys eight bits at a time
+// from the top, each round counting the candidates that agree with the k-th so far by their next eight bits; then, where several share the
+// k-th's key, their places likewise.  low: a key that none is below; bits: of the largest difference from it.  Returns the least that is left.
+// Called by all threads.
+template <int kWaves, int kRegs>
+__device__ __forceinline__ uint64_t keep_best(uint64_t (&mine)[kRegs], int k, uint32_t low, int bits, PickSpace& ws, int tid) {
+    const int lane = tid & 63;
+    int need = k, round = 0;
+    for (int i = tid; i < 256; i += 64 * kWaves) ws.bins[0][i] = 0;
     __syncthreads();
-    for (int k = 2; k <= size; k <<= 1)
-        for (int j = k >> 1; j > 0; j >>= 1) {
-            for (int p = tid; p < size / 2; p += kThreads) {
-                const int i = 2 * p - (p & (j - 1)), other = i + j;
-                const uint64_t a = list[i], b = list[other];
-                if ((a < b) == ((i & k) == 0)) {
-                    list[i] = b;
-                    list[other] = a;
-                }
+    // The k-th of digits(i), whose `shift` lowest bits are open where that is enough to tell the k best.
+    auto find = [&](auto digits, auto counts, int& shift) {
+        uint32_t prefix = 0;
+        for (;; ++round) {
+            const int width = shift < 8 ? shift : 8;
+            shift -= width;
+            uint32_t* const bins = ws.bins[round % 3];
+#pragma unroll
+            for (int i = 0; i < kRegs; ++i) {
+                const uint32_t d = digits(i) >> shift;
+                if (counts(i) && d >> width == prefix) atomicAdd(bins + (d & ((1u << width) - 1)), 1u);
             }
+            for (int i = tid; i < 256; i += 64 * kWaves) ws.bins[(round + 1) % 3][i] = 0;
             __syncthreads();
+            // Lane l has the bins 255 - 4 l and the three below: the scan counts from the top.
+            const int first = 252 - 4 * lane;
+            int n[4], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                n[i] = (int)bins[first + 3 - i];
+                sum += n[i];
+            }
+            const int higher = wave_incl_scan_i(sum) - sum;
+            const unsigned long long hit = __ballot(higher < need && higher + sum >= need);
+            const int at = __builtin_ctzll(hit | 1ull << 63);
+            int above = higher, digit = first + 3, count = n[0];
+#pragma unroll
+            for (int i = 1; i < 4; ++i)
+                if (above + count < need) {
+                    above += count;
+                    count = n[i];
+                    digit = first + 3 - i;
+                }
+            need -= __builtin_amdgcn_readlane(above, at);
+            count = __builtin_amdgcn_readlane(count, at);
+            prefix = prefix << width | (uint32_t)__builtin_amdgcn_readlane(digit, at);
+            if (count == need || shift == 0) {
+                ++round;
+                if (count == need) need = 0;
+                return prefix << shift;
+            }
         }
+    };
+    int shift = bits;
+    const uint32_t key = low + find([&](int i) { return (uint32_t)(mine[i] >> 32) - low; }, [&](int i) { return mine[i] != 0; }, shift);
+    uint64_t least = (uint64_t)key << 32;
+    if (need > 0) {
+        shift = 32;
+        least |= find([&](int i) { return (uint32_t)mine[i]; }, [&](int i) { return (uint32_t)(mine[i] >> 32) == key; }, shift);
+    }
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) mine[i] = mine[i] >= least ? mine[i] : 0;
+    __syncthreads();
+    return least;
 }
 
+// How many candidates are kept where k are asked for: what ranking or the bitonic network below takes.
+template <int kWaves>
+__device__ __forceinline__ int most_kept(int k) { return kWaves < kRowWaves || k <= 128 ? 128 : kMaxTopK; }
+
+template <int kRegs>
+__device__ __forceinline__ int count_all(const uint64_t (&mine)[kRegs]) {      // the wave's
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) n += __builtin_popcountll(__ballot(mine[i] != 0));
+    return n;
+}
+// How many of the list's n candidates are better; it goes on with up to 7 zeros.
+__device__ __forceinline__ int rank_of(uint64_t c, const uint64_t* list, int n) {
+    int rank = 0;
+    for (int j = 0; j < n; j += 8) {
+        uint64_t y[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = list[j + i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) rank += y[i] > c;
+    }
+    return rank;
+}
+
+// Puts the threads' candidates (0: none; `kept` of them in the wave), or the k best where they are more than most_kept(k), into ws.list, in no order, and returns
+// how many there are.  least: none is below, raised to the least of the k best; bits: of the largest difference of a key from that one's.  Called by all threads, which find the list ready.
+template <int kWaves, int kRegs>
+__device__ __forceinline__ int gather_best(uint64_t (&mine)[kRegs], int kept, int k, uint64_t& least, int bits, PickSpace& ws, int tid) {
+    const int lane = tid & 63, wave = uniform(tid >> 6);
+    int n = 0, at = 0;
+    for (bool again = true;; again = false) {
+        if (lane == 0) ws.counts[wave] = kept;
+        __syncthreads();
+        n = at = 0;
+#pragma unroll
+        for (int i = 0; i < kWaves; ++i) {
+            at += i < wave ? ws.counts[i] : 0;
+            n += ws.counts[i];
+        }
+        n = uniform(n);
+        if (!again || n <= most_kept<kWaves>(k)) break;
+        least = keep_best<kWaves, kRegs>(mine, k, (uint32_t)(least >> 32), bits, ws, tid);
+        kept = count_all(mine);
+    }
+    at = uniform(at);
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) {
+        const unsigned long long here = __ballot(mine[i] != 0);
+        if (here == 0) continue;
+        if (mine[i] != 0) ws.list[at + before(here)] = mine[i];
+        at += __builtin_popcountll(here);
+    }
+    if (n <= 128 && tid < 8) ws.list[n + tid] = 0;      // ranks are counted eight at a time
+    __syncthreads();
+    return n;
+}
+
+// The value of lane `this one ^ kJ`.
+template <int kJ>
+__device__ __forceinline__ uint32_t other_lane(uint32_t x, int lane) {
+    if constexpr (kJ == 1) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true);         // quad_perm [1,0,3,2]
+    else if constexpr (kJ == 2) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, true);    // quad_perm [2,3,0,1]
+    else if constexpr (kJ == 4) return (uint32_t)__builtin_amdgcn_ds_swizzle((int)x, 4 << 10 | 0x1f);
+    else if constexpr (kJ == 8) return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x128, 0xf, 0xf, true);   // row_ror:8
+    else {
+        const u32x2_t t = kJ == 16 ? __builtin_amdgcn_permlane16_swap(x, x, false, false) : __builtin_amdgcn_permlane32_swap(x, x, false, false);
+        const uint32_t t0 = t.x, t1 = t.y;
+        return lane & kJ ? t0 : t1;
+    }
+}
+// The last steps of a bitonic merge of runs of kSize lanes; descending where `down`.
+template <int kSize>
+__device__ __forceinline__ void sort_step(uint64_t& x, int lane, bool down) {
+    if constexpr (kSize > 1) {
+        constexpr int kJ = kSize / 2;
+        const uint64_t y = (uint64_t)other_lane<kJ>((uint32_t)(x >> 32), lane) << 32 | other_lane<kJ>((uint32_t)x, lane);
+        x = (x > y) == (down == ((lane & kJ) == 0)) ? x : y;
+        sort_step<kJ>(x, lane, down);
+    }
+}
+
+// Calls put(rank, candidate) for every one of the threads' candidates, or for the best of them, k at least; returns how many
+// it was called for.  Called by all threads, which are done with ws.list.
+template <int kWaves, int kRegs, typename Put>
+__device__ __forceinline__ int rank_candidates(uint64_t (&mine)[kRegs], int k, uint64_t least, int bits, PickSpace& ws, int tid, Put put) {
+    const int lane = tid & 63, wave = uniform(tid >> 6);
+    const int n = gather_best<kWaves, kRegs>(mine, count_all(mine), k, least, bits, ws, tid);
+    if (n <= 128) {
+        if (tid < 128 && wave * 64 < n) {
+            const uint64_t x = tid < n ? ws.list[tid] : 0;
+            const int rank = rank_of(x, ws.list, n);
+            if (tid < n) put(rank, x);
+        }
+        return n;
+    }
+    // A bitonic network, a candidate per thread: steps within a wave by lane exchanges, the six others through LDS.
+    if constexpr (kWaves == kRowWaves) {
+        uint64_t x = tid < n ? ws.list[tid] : 0;
+        sort_step<2>(x, lane, (tid & 2) == 0);
+        sort_step<4>(x, lane, (tid & 4) == 0);
+        sort_step<8>(x, lane, (tid & 8) == 0);
+        sort_step<16>(x, lane, (tid & 16) == 0);
+        sort_step<32>(x, lane, (tid & 32) == 0);
+        sort_step<64>(x, lane, (tid & 64) == 0);
+        for (int size = 128; size <= kMaxTopK; size <<= 1) {
+            for (int j = size >> 1; j >= 64; j >>= 1) {
+                __syncthreads();
+                ws.list[tid] = x;
+                __syncthreads();
+                const uint64_t y = ws.list[tid ^ j];
+                x = (x > y) == (((tid & size) == 0) == ((tid & j) == 0)) ? x : y;
+            }
+            sort_step<64>(x, lane, (tid & size) == 0);
+        }
+        if (tid < n) put(tid, x);
+    }
+    return n;
+}
+
+// The row's token and its logit, fetched ahead by the thread that writes what becomes of them.
+struct Token {
+    int id;
+    float x;
+};
 template <typename T>
-__device__ __forceinline__ void write_sums(const LogprobsParams& prm, int row, const Sums& a, float log_s, int tid) {
+__device__ __forceinline__ Token fetch_token(const LogprobsParams& prm, int row, int tid) {
+    Token t = {-1, __builtin_nanf("")};
+    if (tid == 0 && prm.tokens) {
+        t.id = prm.tokens[row];
+        if (t.id >= 0 && t.id < prm.vocab) t.x = to_float(static_cast<const T*>(prm.logits)[row * prm.row_stride + t.id]);
+    }
+    return t;
+}
+__device__ __forceinline__ void write_sums(const LogprobsParams& prm, int row, const Sums& a, float log_s, const Token& token, int tid) {
     if (tid != 0) return;
     if (prm.lse) prm.lse[row] = a.m * prm.scale + log_s;
     if (prm.entropy) prm.entropy[row] = log_s - a.t / a.s * kLn2;
-    if (prm.tokens) {
-        const int token = prm.tokens[row];
-        float lp = 0.0f;
-        if (token >= 0) {
-            const float x = token < prm.vocab ? to_float(static_cast<const T*>(prm.logits)[row * prm.row_stride + token]) : __builtin_nanf("");
-            lp = (x - a.m) * prm.scale - log_s;
-        }
-        prm.token_lp[row] = lp;
-    }
+    if (prm.token_lp) prm.token_lp[row] = token.id < 0 ? 0.0f : (token.x - a.m) * prm.scale - log_s;
 }
-__device__ __forceinline__ void write_top(const LogprobsParams& prm, int row, const uint64_t* list, int n, float m, float log_s, int tid, int threads) {
-    for (int i = tid; i < prm.top_k; i += threads) {
-        const uint64_t c = i < n ? list[i] : 0;
-        const int64_t at = (int64_t)row * prm.top_k + i;
-        prm.top_tok[at] = c ? (int)~(uint32_t)c : -1;
-        prm.top_lp[at] = c ? (key_value((uint32_t)(c >> 32)) - m) * prm.scale - log_s : __builtin_nanf("");
-    }
+__device__ __forceinline__ void write_candidate(const LogprobsParams& prm, int row, int rank, uint64_t c, float m, float log_s) {
+    if (rank >= prm.top_k) return;
+    const int64_t at = (int64_t)row * prm.top_k + rank;
+    prm.top_tok[at] = c ? (int)~(uint32_t)c : -1;
+    prm.top_lp[at] = c ? (key_value((uint32_t)(c >> 32)) - m) * prm.scale - log_s : __builtin_nanf("");
 }
 
 // What a part of a row leaves in the workspace: its sums, and its candidates in order (0: none).
@@ -192,115 +368,137 @@ __device__ __host__ __forceinline__ PartSpace part_space(char* ws, int rows, int
     return PartSpace{reinterpret_cast<float*>(ws), reinterpret_cast<uint64_t*>(ws + (size_t)rows * parts * 16)};
 }
 
-// A row, or one of its parts, per workgroup.  kCap: candidates that a wave's list holds; 0 without alternatives.
-template <typename T, int kCap>
-__global__ __launch_bounds__(kRowThreads) void logprobs_kernel(LogprobsParams prm, int parts, int part_size) {
-    __shared__ uint64_t lists[kCap ? kRowWaves * kCap : 1];
-    __shared__ volatile uint32_t taus[kRowWaves];
-    __shared__ int counts[kRowWaves];
-    __shared__ float tops[kRowWaves];
-    __shared__ Sums partial[kRowWaves];
+// A row, or one of its parts, per workgroup.  kCap: chunks that a wave's list holds; 0 without alternatives, kAtOnce for alternatives of
+// rows (or parts) of one round, whose values stay in registers.
+template <typename T, int kCap, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, 4) void logprobs_kernel(LogprobsParams prm, int parts, int part_size) {
+    constexpr bool kTop = kCap != 0, kList = kCap > 0;
+    __shared__ uint64_t lists[kList ? kWaves * kCap : 1];
+    __shared__ uint32_t taus[kWaves];
+    __shared__ typename std::conditional<kTop, PickSpace, int>::type ws;
+    __shared__ float tops[kWaves];
+    __shared__ Sums partial[kWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int row = blockIdx.x / (unsigned)parts, part = blockIdx.x - row * parts;
     const int begin = part * part_size, end = prm.vocab - begin < part_size ? prm.vocab : begin + part_size;
     const T* const logits = static_cast<const T*>(prm.logits) + row * prm.row_stride;
     const float c = prm.scale_log2;
-    const int k = prm.top_k, per_wave = (k + kRowWaves - 1) / kRowWaves;
-    uint64_t* const list = lists + wave * kCap;
+    const int k = prm.top_k;
+    const Token token = parts == 1 ? fetch_token<T>(prm, row, tid) : Token{};
+    // per_wave values of each of `enough` waves are k values: tau is what the enough-th best of the waves has per_wave of.
+    const int with_values = (end - begin + kStep - 1) / kStep < kWaves ? (end - begin + kStep - 1) / kStep : kWaves;
+    const int per_wave = (k + with_values - 1) / with_values, enough = per_wave > 0 ? (k + per_wave - 1) / per_wave : 0;
+    uint64_t* const list = lists + (kList ? wave * kCap : 0);
 
     Sums a = {-kFar, 0.0f, 0.0f};
     float top = kNegInf;             // the lane's maximum
     uint32_t tau = 1, own = 1;       // least key to take: by all waves' maxima, by the own list
-    int count = 0, round = 0;
-    if (tid < kRowWaves) taus[tid] = 0;
-    __syncthreads();
-
+    int count = 0;
     // Largest keys so far -> tau.  The waves do not wait for each other: an older tau is a lower one.
     auto raise = [&]() {
-        const uint32_t mine = nth_key(order_key(top), per_wave);
-        if (lane == 0) taus[wave] = mine;
+        const uint32_t mine = wave < with_values ? nth_key(top, per_wave) : 0u;
+        if (lane == 0) __hip_atomic_store(taus + wave, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     };
     auto look = [&]() {
-        uint32_t all = ~0u;
+        // (The last three bits, made the wave's, keep them apart.)
+        const uint32_t mine = lane < kWaves ? (__hip_atomic_load(taus + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) & ~7u) | (uint32_t)lane : 0u;
+        int better = 0;
 #pragma unroll
-        for (int i = 0; i < kRowWaves; ++i) {
-            const uint32_t x = taus[i];
-            all = x < all ? x : all;
-        }
-        all = (uint32_t)uniform((int)all);
+        for (int i = 0; i < kWaves; ++i) better += (uint32_t)__builtin_amdgcn_readlane((int)mine, i) > mine;
+        const unsigned long long at = __ballot(lane < kWaves && better == enough - 1);
+        const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)mine, __builtin_ctzll(at | 1ull << 63)) & ~7u;
         tau = all > tau ? all : tau;
     };
-    const int stride = kRowWaves * kLoads * kStep, rounds = (end - begin + stride - 1) / stride;
-    for (; round < rounds; ++round) {
-        const int base = begin + round * stride + wave * (kLoads * kStep);
-        Raw<T> raw[kLoads];
-        float x[kLoads][kVec], most[kLoads];
-        if (base + kLoads * kStep <= end) {
+    // A round: kLoads steps per wave, the waves side by side in each, so that a short row has values for all, and a wave's rounds come in
+    // order of their indices.  A chunk that would pass the row's end is read at the end, and its values that belong to the chunk
+    // before it (`skip` of them, all if it lies behind the end) are left out.
+    constexpr int kRound = kWaves * kLoads * kStep, kChunk = Chunk<T>::kCount, kChunks = kVals / kChunk, kPerStep = kStep / 64 / kChunk;
+    const int rounds = (end - begin + kRound - 1) / kRound;
+    auto nominal = [&](int round, int q) {
+        return begin + round * kRound + ((q / kPerStep) * kWaves + wave) * kStep + (q % kPerStep) * (64 * kChunk) + lane * kChunk;
+    };
+    const bool tiny = prm.vocab < kChunk;      // no chunk fits: the first thread takes the values one by one
+    const int last = begin + (rounds - 1) * kRound < end - kChunk ? begin + (rounds - 1) * kRound : end - kChunk;      // where the last round reads from
+    Chunk<T> next[kChunks];
+    uint32_t ahead[kChunks];                   // of a round's chunks, in bytes
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) raw[u].load(logits + base + u * kStep + lane * kVec);
+    for (int q = 0; q < kChunks; ++q) ahead[q] = (uint32_t)(nominal(0, q) - begin) * (uint32_t)sizeof(T);
+    auto fetch = [&](int round) {
+        int from = begin + round * kRound;
+        if (round == rounds - 1) {
+            from = last;
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u)
+            for (int q = 0; q < kChunks; ++q) {
+                const int at = nominal(round, q) < end - kChunk ? nominal(round, q) : end - kChunk;
+                ahead[q] = (uint32_t)(at - last) * (uint32_t)sizeof(T);
+            }
+        }
+        const char* const base = reinterpret_cast<const char*>(logits + from);
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) x[u][i] = raw[u].get(i);
+        for (int q = 0; q < kChunks; ++q) next[q].load(reinterpret_cast<const T*>(base + ahead[q]));
+    };
+    float x[kVals];
+    for (int round = 0; round < rounds; ++round) {
+        if (tiny) {
+#pragma unroll
+            for (int i = 0; i < kVals; ++i) x[i] = tid == 0 && i < end ? to_float(logits[i]) : kNegInf;
         } else {
+            fetch(round);
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u)
+            for (int i = 0; i < kVals; ++i) x[i] = next[i / kChunk].get(i % kChunk);
+            if (round + 1 == rounds) {
 #pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    const int at = base + u * kStep + lane * kVec + i;
-                    x[u][i] = at < end ? to_float(logits[at]) : kNegInf;
+                for (int q = 0; q < kChunks; ++q) {
+                    const int skip = nominal(round, q) - (last + (int)(ahead[q] / (uint32_t)sizeof(T)));
+#pragma unroll
+                    for (int i = 0; i < kChunk; ++i) x[q * kChunk + i] = i < skip ? kNegInf : x[q * kChunk + i];
                 }
+            }
         }
-        float new_top = top;
+        float most[kChunks], all = kNegInf;
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u) {
-            most[u] = x[u][0];
+        for (int q = 0; q < kChunks; ++q) {
+            most[q] = x[q * kChunk];
 #pragma unroll
-            for (int i = 1; i < kVec; ++i) most[u] = fmaxf(most[u], x[u][i]);
-            new_top = fmaxf(new_top, most[u]);
+            for (int i = 1; i < kChunk; ++i) most[q] = fmaxf(most[q], x[q * kChunk + i]);
+            all = fmaxf(all, most[q]);
         }
-        if (__ballot(new_top > top) != 0) {
-            top = new_top;
+        if (__ballot(all > top) != 0) {
+            top = fmaxf(top, all);
             move_to(a, fmaxf(top, -kFar), c);
         }
         const float mc = a.m * c;
 #pragma unroll
-        for (int u = 0; u < kLoads; ++u)
-#pragma unroll
-            for (int i = 0; i < kVec; ++i) add(a, __builtin_fmaf(x[u][i], c, -mc));
-        if constexpr (kCap > 0) {
-            if ((round & (round - 1)) == 0) {      // rounds 0, 1, 2, 4, 8, ...
+        for (int i = 0; i < kVals; ++i) add(a, __builtin_fmaf(x[i], c, -mc));
+        if constexpr (kList) {
+            if ((round & (round - 1)) == 0 && (round & 0x2aaaaaaa) == 0) {      // rounds 0, 1, 4, 16, ...
                 raise();
                 if (round == 0) __syncthreads();
                 look();
             }
+            const uint32_t low = tau > own ? tau : own;
+            const float low_value = key_value(low);
+            const bool any = low <= kLowKey;       // -inf counts, and what is left out has to be told from it
+            if (!any && __ballot(all >= low_value) == 0) continue;
 #pragma unroll
-            for (int u = 0; u < kLoads; ++u) {
-                const uint32_t low = tau > own ? tau : own;
-                if (low > kLowKey && __ballot(most[u] >= key_value(low)) == 0) continue;
-                const int first = base + u * kStep + lane * kVec;
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    const uint32_t key = order_key(x[u][i]);
-                    const bool take = key >= low && first + i < end;
-                    const unsigned long long takes = __ballot(take);
-                    if (takes == 0) continue;
-                    if (count + 64 > kCap) {
-                        // The list's k best come before any later value that equals the least of them; not before the rest
-                        // of these 512, whose indices are not in order, hence `low`.
-                        const uint32_t least = (uint32_t)(cut_list<kCap>(list, count, k, lane) >> 32);
-                        own = least + 1;
-                        count = k;
-                    }
-                    if (take) list[count + __builtin_popcountll(takes & ((1ull << lane) - 1))] = candidate(key, first + i);
-                    count += __builtin_popcountll(takes);
+            for (int q = 0; q < kChunks; ++q) {
+                const unsigned long long takes =
+                    any ? __ballot(order_key(most[q]) >= low && nominal(round, q) < end) : __ballot(most[q] >= low_value);
+                if (takes == 0) continue;
+                if (count + 64 > kCap) {
+                    // The k best chunks come before any of a later round whose maximum equals the least of them; not before the rest of
+                    // this one, which are not in order: `low` stays.
+                    own = (uint32_t)(cut_list<kCap>(list, count, k, lane) >> 32) + 1;
+                    count = k;
                 }
+                if (takes >> lane & 1) list[count + before(takes)] = candidate(order_key(most[q]), nominal(round, q));
+                count += __builtin_popcountll(takes);
             }
         }
     }
 
     // The lanes' sums, then the waves'.
-    if constexpr (kCap > 0) raise();
+    if constexpr (kTop) raise();
     const float wave_top = wave_max(top);
     {
         const float m = fmaxf(wave_top, -kFar);
@@ -315,10 +513,10 @@ __global__ __launch_bounds__(kRowThreads) void logprobs_kernel(LogprobsParams pr
     __syncthreads();
     float row_top = tops[0];
 #pragma unroll
-    for (int i = 1; i < kRowWaves; ++i) row_top = fmaxf(row_top, tops[i]);
+    for (int i = 1; i < kWaves; ++i) row_top = fmaxf(row_top, tops[i]);
     Sums r = {fmaxf(row_top, -kFar), 0.0f, 0.0f};
 #pragma unroll
-    for (int i = 0; i < kRowWaves; ++i) {
+    for (int i = 0; i < kWaves; ++i) {
         Sums x = partial[i];
         move_to(x, r.m, c);
         r.s += x.s;
@@ -327,117 +525,145 @@ __global__ __launch_bounds__(kRowThreads) void logprobs_kernel(LogprobsParams pr
     if (__builtin_fabsf(row_top) >= kFar && __builtin_fabsf(row_top) < __builtin_inff()) {
         __syncthreads();
         a = Sums{row_top, 0.0f, 0.0f};
-        for (int i = begin + tid; i < end; i += kRowThreads) add(a, (to_float(logits[i]) - row_top) * c);
+        for (int i = begin + tid; i < end; i += 64 * kWaves) add(a, (to_float(logits[i]) - row_top) * c);
         a.s = wave_sum(a.s);
         a.t = wave_sum(a.t);
         if (lane == 0) partial[wave] = a;
         __syncthreads();
         r = Sums{row_top, 0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < kRowWaves; ++i) {
+        for (int i = 0; i < kWaves; ++i) {
             r.s += partial[i].s;
             r.t += partial[i].t;
         }
     }
 
-    int n = 0;
-    if constexpr (kCap > 0) {
-        look();
-        // All candidates from tau on, one behind the other.
-        uint64_t mine[kCap / 64];
-        int kept = 0;
-#pragma unroll
-        for (int i = 0; i < kCap / 64; ++i) {
-            mine[i] = 64 * i + lane < count ? list[64 * i + lane] : 0;
-            if ((uint32_t)(mine[i] >> 32) < tau) mine[i] = 0;
-            kept += __builtin_popcountll(__ballot(mine[i] != 0));
-        }
-        if (lane == 0) counts[wave] = kept;
-        __syncthreads();
-        int at = 0;
-#pragma unroll
-        for (int i = 0; i < kRowWaves; ++i) {
-            at += i < wave ? counts[i] : 0;
-            n += counts[i];
-        }
-        at = uniform(at);
-#pragma unroll
-        for (int i = 0; i < kCap / 64; ++i) {
-            const unsigned long long here = __ballot(mine[i] != 0);
-            if (mine[i] != 0) lists[at + __builtin_popcountll(here & ((1ull << lane) - 1))] = mine[i];
-            at += __builtin_popcountll(here);
-        }
-        __syncthreads();
-        sort_candidates<kRowThreads>(lists, n, kRowWaves * kCap, tid);
-    }
-    if (parts > 1) {
-        const PartSpace ws = part_space(prm.workspace, prm.rows, parts);
-        if (tid == 0) *reinterpret_cast<f32x4_t*>(ws.sums + 4 * (int64_t)blockIdx.x) = f32x4_t{row_top, r.s, r.t, 0.0f};
-        if constexpr (kCap > 0)
-            for (int i = tid; i < k; i += kRowThreads) ws.candidates[(int64_t)blockIdx.x * k + i] = i < n ? lists[i] : 0;
-        return;
-    }
     const float log_s = __builtin_amdgcn_logf(r.s) * kLn2;
-    write_sums<T>(prm, row, r, log_s, tid);
-    if constexpr (kCap > 0) write_top(prm, row, lists, n, r.m, log_s, tid, kRowThreads);
+    const PartSpace to = part_space(prm.workspace, prm.rows, parts);
+    if (parts == 1) write_sums(prm, row, r, log_s, token, tid);
+    else if (tid == 0) *reinterpret_cast<f32x4_t*>(to.sums + 4 * (int64_t)blockIdx.x) = f32x4_t{row_top, r.s, r.t, 0.0f};
+    if constexpr (kTop) {
+        look();
+        uint64_t least = (uint64_t)tau << 32;
+        const int bits = 32 - __builtin_clz((order_key(row_top) - tau) | 1);
+        auto put = [&](int rank, uint64_t c) {
+            if (parts == 1) write_candidate(prm, row, rank, c, r.m, log_s);
+            else if (rank < k) to.candidates[(int64_t)blockIdx.x * k + rank] = c;
+        };
+        if constexpr (!kList) {
+            uint64_t value[kVals];
+#pragma unroll
+            for (int i = 0; i < kVals; ++i) {
+                const int q = i / kChunk, from = tiny ? 0 : last + (int)(ahead[q] / (uint32_t)sizeof(T)), at = from + i % kChunk;
+                const uint32_t key = order_key(x[i]);
+                value[i] = key >= tau && nominal(0, q) < end && at >= nominal(0, q) && at < end ? candidate(key, at) : 0;
+            }
+            const int n = rank_candidates<kWaves, kVals>(value, k, least, bits, ws, tid, put);
+            for (int i = n + tid; i < k; i += 64 * kWaves) put(i, 0);
+            return;
+        } else {
+            uint64_t mine[kCap / 64];
+#pragma unroll
+            for (int i = 0; i < kCap / 64; ++i) {
+                mine[i] = 64 * i + lane < count ? list[64 * i + lane] : 0;
+                if ((uint32_t)(mine[i] >> 32) < tau) mine[i] = 0;
+            }
+            const int chunks = gather_best<kWaves, kCap / 64>(mine, count_all(mine), k, least, bits, ws, tid);
+            least &= ~0xffffffffull;      // places of chunks are not places of values
+            // The chunks' values, a chunk per thread.
+            static_assert(64 * kRowWaves >= kMaxTopK, "a thread for every chunk");
+            const int first = tid < chunks ? (int)~(uint32_t)ws.list[tid] : end, from = first < end - kChunk ? first : end - kChunk;
+            Chunk<T> chunk;
+            chunk.load(logits + from);
+            uint64_t value[kChunk];
+#pragma unroll
+            for (int i = 0; i < kChunk; ++i) {
+                const uint64_t c = candidate(order_key(chunk.get(i)), from + i);
+                value[i] = from + i >= first && from + i < end && c >= least && c >> 32 != 0 ? c : 0;
+            }
+            const int n = rank_candidates<kWaves, kChunk>(value, k, least, bits, ws, tid, put);
+            for (int i = n + tid; i < k; i += 64 * kWaves) put(i, 0);
+        }
+    }
 }
 
 // A row's parts put together, a workgroup per row.
 template <typename T>
-__global__ __launch_bounds__(kRowThreads) void logprobs_merge_kernel(LogprobsParams prm, int parts) {
-    __shared__ uint64_t list[kMostMerged];
-    __shared__ int total;
-    const int tid = threadIdx.x, row = blockIdx.x, k = prm.top_k;
-    const PartSpace ws = part_space(prm.workspace, prm.rows, parts);
-    const float* const sums = ws.sums + (int64_t)row * parts * 4;
-    const uint64_t* const from = ws.candidates + (int64_t)row * parts * k;
-    Sums r = {kNegInf, 0.0f, 0.0f};
-    uint64_t least = 1;              // k candidates of one part are that good
-    for (int p = 0; p < parts; ++p) {
-        r.m = fmaxf(r.m, sums[4 * p]);
+__global__ __launch_bounds__(64 * kRowWaves) void logprobs_merge_kernel(LogprobsParams prm, int parts) {
+    __shared__ PickSpace ws;
+    const int tid = threadIdx.x, lane = tid & 63, row = blockIdx.x, k = prm.top_k;
+    const PartSpace from = part_space(prm.workspace, prm.rows, parts);
+    const Token token = fetch_token<T>(prm, row, tid);
+    const float* const sums = from.sums + (int64_t)row * parts * 4;
+    const uint64_t* const candidates = from.candidates + (int64_t)row * parts * k;
+    constexpr int kRegs = kMostMerged / (64 * kRowWaves);
+    uint64_t mine[kRegs];
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) mine[i] = i * 64 * kRowWaves + tid < parts * k ? candidates[i * 64 * kRowWaves + tid] : 0;
+    // Every wave by itself, a part per lane.
+    float top = kNegInf;
+    uint64_t least = 1, best = 0;    // k candidates of one part are that good; the best one
+    for (int p = lane; p < parts; p += 64) {
+        top = fmaxf(top, sums[4 * p]);
         if (k > 0) {
-            const uint64_t last = from[(int64_t)p * k + k - 1];
+            const uint64_t first = candidates[(int64_t)p * k], last = candidates[(int64_t)p * k + k - 1];
             least = last > least ? last : least;
+            best = first > best ? first : best;
         }
     }
-    for (int p = 0; p < parts; ++p) {
+    Sums r = {wave_max(top), 0.0f, 0.0f};
+    for (int p = lane; p < parts; p += 64) {
         Sums x = {sums[4 * p], sums[4 * p + 1], sums[4 * p + 2]};
         move_to(x, r.m, prm.scale_log2);
         r.s += x.s;
         r.t += x.t;
     }
+    r.s = wave_sum(r.s);
+    r.t = wave_sum(r.t);
     const float log_s = __builtin_amdgcn_logf(r.s) * kLn2;
-    write_sums<T>(prm, row, r, log_s, tid);
+    write_sums(prm, row, r, log_s, token, tid);
     if (k == 0) return;
-    if (tid == 0) total = 0;
-    __syncthreads();
-    for (int i = tid; i < parts * k; i += kRowThreads) {
-        const uint64_t c = from[i];
-        if (c >= least) list[atomicAdd(&total, 1)] = c;
+#pragma unroll
+    for (int j = 32; j > 0; j >>= 1) {
+        const uint64_t l = __shfl_xor(least, j, 64), b = __shfl_xor(best, j, 64);
+        least = l > least ? l : least;
+        best = b > best ? b : best;
     }
-    __syncthreads();
-    const int n = total;
-    sort_candidates<kRowThreads>(list, n, kMostMerged, tid);
-    write_top(prm, row, list, n, r.m, log_s, tid, kRowThreads);
+#pragma unroll
+    for (int i = 0; i < kRegs; ++i) mine[i] = mine[i] >= least ? mine[i] : 0;
+    auto put = [&](int rank, uint64_t x) { write_candidate(prm, row, rank, x, r.m, log_s); };
+    const int n = rank_candidates<kRowWaves, kRegs>(mine, k, least, 32 - __builtin_clz((uint32_t)(best >> 32) - (uint32_t)(least >> 32) | 1), ws, tid, put);
+    for (int i = n + tid; i < k; i += 64 * kRowWaves) put(i, 0);
 }
 
 template <typename T>
 hipError_t launch_type(const LogprobsParams& prm, const LogprobsCut& cut, hipStream_t stream) {
     const dim3 grid((unsigned)((int64_t)prm.rows * cut.parts));
+    auto with = [&](auto cap, auto waves) {
+        constexpr int kCap = decltype(cap)::value, kWaves = decltype(waves)::value;
+        return launch(logprobs_kernel<T, kCap, kWaves>, grid, 64 * kWaves, stream, prm, cut.parts, cut.part_size);
+    };
+    const std::integral_constant<int, kRowWaves> many;
+    const std::integral_constant<int, kFewWaves> few;
+    const bool is_short = cut.parts == 1 && prm.vocab <= kFewWaves * kLoads * kStep, at_once = cut.part_size <= kAtOnceSize;
     hipError_t e;
-    if (prm.top_k == 0) e = launch(logprobs_kernel<T, 0>, grid, kRowThreads, stream, prm, cut.parts, cut.part_size);
-    else if (prm.top_k <= 64) e = launch(logprobs_kernel<T, 256>, grid, kRowThreads, stream, prm, cut.parts, cut.part_size);
-    else e = launch(logprobs_kernel<T, 1024>, grid, kRowThreads, stream, prm, cut.parts, cut.part_size);
+    if (prm.top_k == 0) e = is_short ? with(std::integral_constant<int, 0>(), few) : with(std::integral_constant<int, 0>(), many);
+    else if (is_short && prm.top_k <= 128) e = with(std::integral_constant<int, kAtOnce>(), few);
+    else if (at_once) e = with(std::integral_constant<int, kAtOnce>(), many);
+    else if (prm.top_k <= 64) e = with(std::integral_constant<int, 256>(), many);
+    else e = with(std::integral_constant<int, 640>(), many);
     if (e != hipSuccess || cut.parts == 1) return e;
-    return launch(logprobs_merge_kernel<T>, dim3((unsigned)prm.rows), kRowThreads, stream, prm, cut.parts);
+    return launch(logprobs_merge_kernel<T>, dim3((unsigned)prm.rows), 64 * kRowWaves, stream, prm, cut.parts);
 }
 
 }  // namespace
 
 LogprobsCut logprobs_cut(int rows, int vocab, int top_k) {
-    int parts = 512 / rows;
-    if (parts > vocab / kLeastPart) parts = vocab / kLeastPart;
+    // A round is kAtOnceSize values and takes a workgroup about 1 us, putting parts together 6 to 8 us (a second launch).
+    const int at_once = (vocab + kAtOnceSize - 1) / kAtOnceSize;
+    int parts = kParts / rows < at_once ? kParts / rows : at_once;
     if (top_k > 0 && parts > kMostMerged / top_k) parts = kMostMerged / top_k;
+    if (at_once <= kFewRounds) parts = 1;
     if (parts <= 1) return LogprobsCut{1, vocab, 0};
     const int steps = (vocab + kStep - 1) / kStep, size = (steps + parts - 1) / parts * kStep;
     parts = (vocab + size - 1) / size;
