@@ -20,10 +20,12 @@ struct PrefillParams {
     uint32_t q_and, q_xor;           // applied to pairs of Q's values: a negative scale's sign, a zero scale
     uint16_t* out;                   // bf16 [total_q, n_q_heads, 128]
     float* lse;                      // fp32 [total_q, n_q_heads] or null
+    int32_t* table;                  // kPrefillTableBytes: what the merge kernel has to put together
     float* part_ml;                  // fp32 [kPrefillSlots, slot_rows, 2]: reference maximum (log2 domain), sum
     float* part_o;                   // fp32 [kPrefillSlots, slot_rows, 128]
     int slot_rows;
 };
+constexpr size_t kPrefillTableBytes = 32 + 32 * (size_t)kPrefillShares;
 hipError_t launch_prefill(const PrefillParams& prm, hipStream_t stream);
 
 }  // namespace xattn

@@ -29,7 +29,9 @@ constexpr float kSlackLog2 = 8.0f;                    // how far a row's maximum
 struct PrefillWork {
     PrefillSeq s;
     int b, parts, index;      // index: of the work among the sequence's (per KV head)
-    int slot;                 // first slot of the sequence
+    int slot, split;          // of the sequence: first slot, tiles of earlier sequences that are in several parts (per KV head)
+    int splits;               // tiles in several parts, per KV head
+    const char *k, *v;        // the sequence's ranges
     bool found;
 };
 __device__ __forceinline__ PrefillSeq load_seq(const PrefillParams& prm, int b) {
@@ -38,66 +40,109 @@ __device__ __forceinline__ PrefillSeq load_seq(const PrefillParams& prm, int b) 
     const int start = prm.q_starts[i], end = prm.q_starts[i + 1], kv = prm.kv_lens[i];
     return prefill_seq(in ? start : 0, in ? end : 0, in ? kv : 0, prm.total_q, prm.group);
 }
-// What work number j (per KV head) is: of all parts (kMerge false), or of all tiles in several parts (kMerge true).  Lane l has
-// the sequences l << lg ..; one scan finds j's lane, another the sequence among the lane's.
-template <bool kMerge>
+struct Amounts {
+    int work, slots, split;
+};
+__device__ __forceinline__ Amounts amounts_of(const PrefillSeq& s, int share) {
+    const int parts = prefill_parts(s.blocks, share);
+    return Amounts{s.tiles * parts, parts > 1 ? s.tiles * parts : 0, parts > 1 ? s.tiles : 0};
+}
+// What work number j (per KV head) is.  Lane l has the sequences l << lg ..; one scan finds j's lane, another the sequence among the
+// lane's.  Up to 64 sequences, one per lane, are taken in the order of their lengths, longest first: workgroups start in the order of their
+// numbers, and long work that starts late ends late.
 __device__ __forceinline__ PrefillWork find_work(const PrefillParams& prm, int j, int lane) {
     const int lg = prm.batch <= 64 ? 0 : 26 - __builtin_clz((unsigned)(prm.batch - 1));
     const int chunk = 1 << lg;
-    float cost = 0.0f;
-    PrefillSeq s = {};
-    for (int i = 0; i < chunk; ++i) {
-        s = load_seq(prm, (lane << lg) + i);
-        cost += prefill_cost(s);
-    }
-    const int share = prefill_share(wave_sum(cost) * (float)prm.n_kv_heads);
-    auto amounts = [&](const PrefillSeq& q, int& work, int& slots) {
-        const int parts = prefill_parts(q.blocks, share);
-        const int split = parts > 1 ? q.tiles * parts : 0;
-        work = kMerge ? (parts > 1 ? q.tiles : 0) : q.tiles * parts;
-        slots = split;
-        return parts;
-    };
-    int work = 0, slots = 0;
+    PrefillWork r;
+    PrefillSeq s = load_seq(prm, lane << lg);
+    float cost = prefill_cost(s);
+    Amounts mine;
+    int b = lane << lg, share;
+    u32x2_t k = {0u, 0u}, v = {0u, 0u};
     if (chunk == 1) {
-        amounts(s, work, slots);
+        const int i = lane < prm.batch ? lane : 0;
+        k = *reinterpret_cast<const u32x2_t*>(prm.k_ptrs + i);
+        v = *reinterpret_cast<const u32x2_t*>(prm.v_ptrs + i);
+        share = prefill_share(wave_sum(cost) * (float)prm.n_kv_heads);
+        const int key = s.tiles > 0 ? s.blocks : -1;
+        int before = 0;
+        for (int l = 0; l < prm.batch; ++l) {
+            const int other = __builtin_amdgcn_readlane(key, l);
+            before += other > key || (other == key && l < lane);
+        }
+        if (lane >= prm.batch) before = lane;
+        // lane `before` becomes this one's
+        auto to = [&](int x) { return __builtin_amdgcn_ds_permute(before * 4, x); };
+        s = PrefillSeq{to(s.first), to(s.q), to(s.kv), to(s.tiles), to(s.blocks)};
+        b = to(b);
+        mine = amounts_of(s, share);
     } else {
+        for (int i = 1; i < chunk; ++i) cost += prefill_cost(load_seq(prm, (lane << lg) + i));
+        share = prefill_share(wave_sum(cost) * (float)prm.n_kv_heads);
+        mine = Amounts{0, 0, 0};
         for (int i = 0; i < chunk; ++i) {
-            int w, n;
-            amounts(load_seq(prm, (lane << lg) + i), w, n);
-            work += w;
-            slots += n;
+            const Amounts a = amounts_of(load_seq(prm, (lane << lg) + i), share);
+            mine.work += a.work;
+            mine.slots += a.slots;
+            mine.split += a.split;
         }
     }
-    int before = wave_incl_scan_i(work) - work, slots_before = wave_incl_scan_i(slots) - slots;
-    unsigned long long hit = __ballot(j >= before && j < before + work);
-    PrefillWork r;
+    int work = wave_incl_scan_i(mine.work), slots = wave_incl_scan_i(mine.slots), split = wave_incl_scan_i(mine.split);
+    r.splits = __builtin_amdgcn_readlane(split, 63);
+    // Where all work is on its way at once, two workgroups to a compute unit, the later half comes in reverse: long work shares a
+    // compute unit with short work.
+    const int all = __builtin_amdgcn_readlane(work, 63), half = (all + 1) / 2;
+    if (all * prm.n_kv_heads <= kPrefillShares && j >= half && j < all) j = all - 1 - (j - half);
+    unsigned long long hit = __ballot(j >= work - mine.work && j < work);
     r.found = hit != 0;
     int at = hit ? __builtin_ctzll(hit) : 0;
-    r.index = j - __builtin_amdgcn_readlane(before, at);
-    r.slot = __builtin_amdgcn_readlane(slots_before, at);
-    r.b = at;
+    r.index = j - __builtin_amdgcn_readlane(work - mine.work, at);
+    r.slot = __builtin_amdgcn_readlane(slots - mine.slots, at);
+    r.split = __builtin_amdgcn_readlane(split - mine.split, at);
     if (chunk > 1) {
         const int first = at << lg;
-        s = load_seq(prm, lane < chunk ? first + lane : prm.batch);
-        amounts(s, work, slots);
-        before = wave_incl_scan_i(work) - work;
-        slots_before = wave_incl_scan_i(slots) - slots;
-        hit = __ballot(r.index >= before && r.index < before + work);
+        b = first + lane;
+        s = load_seq(prm, lane < chunk ? b : prm.batch);
+        mine = amounts_of(s, share);
+        work = wave_incl_scan_i(mine.work);
+        slots = wave_incl_scan_i(mine.slots);
+        split = wave_incl_scan_i(mine.split);
+        hit = __ballot(r.index >= work - mine.work && r.index < work);
         at = hit ? __builtin_ctzll(hit) : 0;
-        r.index -= __builtin_amdgcn_readlane(before, at);
-        r.slot += __builtin_amdgcn_readlane(slots_before, at);
-        r.b = first + at;
+        r.index -= __builtin_amdgcn_readlane(work - mine.work, at);
+        r.slot += __builtin_amdgcn_readlane(slots - mine.slots, at);
+        r.split += __builtin_amdgcn_readlane(split - mine.split, at);
     }
     r.slot *= prm.n_kv_heads;
+    r.b = __builtin_amdgcn_readlane(b, at);
     r.s.first = __builtin_amdgcn_readlane(s.first, at);
     r.s.q = __builtin_amdgcn_readlane(s.q, at);
     r.s.kv = __builtin_amdgcn_readlane(s.kv, at);
     r.s.tiles = __builtin_amdgcn_readlane(s.tiles, at);
     r.s.blocks = __builtin_amdgcn_readlane(s.blocks, at);
     r.parts = prefill_parts(r.s.blocks, share);
+    if (chunk == 1) {
+        auto lane_ptr = [&](const u32x2_t& x) {
+            return reinterpret_cast<const char*>((uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x.x, r.b) |
+                                                             (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x.y, r.b) << 32));
+        };
+        r.k = lane_ptr(k);
+        r.v = lane_ptr(v);
+    } else if (r.found) {
+        r.k = static_cast<const char*>(uniform(prm.k_ptrs[r.b]));
+        r.v = static_cast<const char*>(uniform(prm.v_ptrs[r.b]));
+    }
     return r;
 }
+
+// For the merge kernel, in the workspace: how many tiles are in several parts, and of each where its rows and its parts are.
+struct SplitTile {
+    int first, q;             // the sequence's packed rows
+    int tile, head, slot, parts;
+    int unused[2];
+};
+__device__ __forceinline__ int* split_count(const PrefillParams& prm) { return prm.table; }
+__device__ __forceinline__ SplitTile* split_tiles(const PrefillParams& prm) { return reinterpret_cast<SplitTile*>(prm.table + 8); }
 
 // ------------------------------------------------------------------------------------------------ blocks
 // Block at key0 of K or V: 1024 chunks of 16 bytes, four per thread, thread t chunk t % 16 of rows t / 16 + 16 i.  The descriptor
@@ -124,7 +169,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int n = lane & 31, hh = lane >> 5;
     const int head = blockIdx.x % (unsigned)prm.n_kv_heads;
-    const PrefillWork w = find_work<false>(prm, (int)(blockIdx.x / (unsigned)prm.n_kv_heads), lane);
+    const PrefillWork w = find_work(prm, (int)(blockIdx.x / (unsigned)prm.n_kv_heads), lane);
+    if (blockIdx.x == 0 && tid == 0) *split_count(prm) = w.splits * prm.n_kv_heads;
     if (!w.found) return;
     // Later tiles see more keys: first.
     const int tile = w.s.tiles - 1 - w.index / w.parts, part = w.index % w.parts;
@@ -132,10 +178,14 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     const int blk0 = part * part_blocks, blk1 = blk0 + part_blocks < blocks ? blk0 + part_blocks : blocks;
     if (part > 0 && blk0 >= blk1) return;
     const bool whole = blocks <= part_blocks;
+    const int first_slot = w.slot + (head * w.s.tiles + tile) * w.parts;
+    if (w.parts > 1 && part == 0 && tid == 0)
+        split_tiles(prm)[(w.split + tile) * prm.n_kv_heads + head] =
+            SplitTile{w.s.first, w.s.q, tile, head, first_slot, whole ? 1 : (blocks + part_blocks - 1) / part_blocks, {0, 0}};
 
     const int row_bytes = prm.n_kv_heads * kRowBytes;
-    const char* const k_head = static_cast<const char*>(uniform(prm.k_ptrs[w.b])) + head * kRowBytes;
-    const char* const v_head = static_cast<const char*>(uniform(prm.v_ptrs[w.b])) + head * kRowBytes;
+    const char* const k_head = w.k + head * kRowBytes;
+    const char* const v_head = w.v + head * kRowBytes;
 
     // This lane's query row.
     const int rows = w.s.q * prm.group, wave_row = tile * kPrefillRows + wave * kWaveRows, row = wave_row + n;
@@ -144,8 +194,8 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     const int64_t q_row = (int64_t)(w.s.first + t) * prm.n_q_heads + h;
     const int lim = row_on ? prefill_visible(w.s, t) : 0;
     const int last_row = wave_row + kWaveRows < rows ? wave_row + kWaveRows - 1 : rows - 1;
-    const int lim_first = prefill_visible(w.s, (int)((unsigned)wave_row / (unsigned)prm.group));
-    const int lim_last = wave_on ? prefill_visible(w.s, (int)((unsigned)last_row / (unsigned)prm.group)) : 0;
+    const int lim_first = uniform(prefill_visible(w.s, (int)((unsigned)wave_row / (unsigned)prm.group)));
+    const int lim_last = uniform(wave_on ? prefill_visible(w.s, (int)((unsigned)last_row / (unsigned)prm.group)) : 0);
 
     bf16x8_t qop[8];
 #pragma unroll
@@ -277,7 +327,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
         if (prm.lse && hh == 0) prm.lse[q_row] = l > 0.0f ? (m + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
         return;
     }
-    const int64_t slot_row = (int64_t)(w.slot + (head * w.s.tiles + tile) * w.parts + part) * prm.slot_rows + wave * kWaveRows + n;
+    const int64_t slot_row = (int64_t)(first_slot + part) * prm.slot_rows + wave * kWaveRows + n;
     float* const to = prm.part_o + slot_row * kHeadDim + 16 * hh;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
@@ -287,43 +337,77 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     if (hh == 0) *reinterpret_cast<f32x2_t*>(prm.part_ml + slot_row * 2) = f32x2_t{m, l};
 }
 
-// The rows of tiles in several parts: blockIdx.x the tile among those, blockIdx.y a quarter of its rows, a wave per row at a
-// time, two columns per lane.
-constexpr int kMergeSplit = 4;
-__global__ __launch_bounds__(256) void prefill_merge_kernel(PrefillParams prm) {
+// The rows of tiles in several parts.  A workgroup takes 16 / kWavesPerRow rows at a time, so many that all workgroups have some: few
+// tiles are in many parts each, whose rows several waves put together.  A lane holds two columns.
+constexpr int kMergeWaves = 16, kMergeGroups = 512;
+__global__ __launch_bounds__(64 * kMergeWaves) void prefill_merge_kernel(PrefillParams prm) {
+    __shared__ f32x2_t sums[kMergeWaves][64];
+    __shared__ f32x2_t tops[kMergeWaves];
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
-    const int head = blockIdx.x % (unsigned)prm.n_kv_heads;
-    const PrefillWork w = find_work<true>(prm, (int)(blockIdx.x / (unsigned)prm.n_kv_heads), lane);
-    if (!w.found) return;
-    const int tile = w.index, part_blocks = prefill_part_blocks(w.s.blocks, w.parts);
-    const int parts = (prefill_tile_blocks(w.s, tile, prm.group) + part_blocks - 1) / part_blocks;
-    if (parts <= 1) return;
-    const int rows = w.s.q * prm.group;
-    const int64_t first_slot = w.slot + (int64_t)(head * w.s.tiles + tile) * w.parts;
-    for (int i = blockIdx.y * (kPrefillRows / kMergeSplit) + wave; i < (int)(blockIdx.y + 1) * (kPrefillRows / kMergeSplit); i += 4) {
-        const int row = tile * kPrefillRows + i;
-        if (row >= rows) return;
-        float top = kLowest;
-        for (int s = lane; s < parts; s += 64) top = fmaxf(top, prm.part_ml[((first_slot + s) * prm.slot_rows + i) * 2]);
-        top = wave_max(top);
-        float l = 0.0f;
+    const int tiles = uniform(*split_count(prm));
+    if (tiles == 0) return;
+    int per_row = 1;          // waves
+    while (per_row < kMergeWaves && tiles * (kPrefillRows / kMergeWaves) * per_row * 2 <= kMergeGroups) per_row *= 2;
+    const int rows_at_once = kMergeWaves / per_row, steps = kPrefillRows / rows_at_once;
+    for (int unit = blockIdx.x; unit < tiles * steps; unit += kMergeGroups) {
+        const SplitTile w = split_tiles(prm)[unit / steps];
+        const int i = unit % steps * rows_at_once + wave / per_row, row = w.tile * kPrefillRows + i, mine = wave % per_row;
+        // (Of bounds in q_starts that do not ascend, an entry may not have been written: nothing outside the buffers then.)
+        const bool known = w.parts > 1 && w.parts <= kPrefillSlots && (unsigned)w.slot <= (unsigned)(kPrefillSlots - w.parts) && (unsigned)w.head < (unsigned)prm.n_kv_heads &&
+                           (unsigned)w.first <= (unsigned)prm.total_q && (unsigned)w.q <= (unsigned)(prm.total_q - w.first) && (unsigned)w.tile < 1u << 24;
+        const bool on = known && row < w.q * prm.group;
+        float top = kLowest, l = 0.0f;
         f32x2_t o = {0.0f, 0.0f};
-        for (int s0 = 0; s0 < parts; s0 += 64) {
-            float by = 0.0f;
-            if (s0 + lane < parts) {
-                const f32x2_t ml = *reinterpret_cast<const f32x2_t*>(prm.part_ml + ((first_slot + s0 + lane) * prm.slot_rows + i) * 2);
-                by = fast_exp2(ml.x - top);
-                l += by * ml.y;
+        if (on) {
+            // Parts mine, mine + per_row, ..., 64 of them at a time.
+            for (int s0 = mine; s0 < w.parts; s0 += 64 * per_row) {
+                const int at = s0 + lane * per_row;
+                f32x2_t ml = {kLowest, 0.0f};
+                if (at < w.parts) ml = *reinterpret_cast<const f32x2_t*>(prm.part_ml + ((int64_t)(w.slot + at) * prm.slot_rows + i) * 2);
+                const float higher = fmaxf(top, wave_max(ml.x)), by = fast_exp2(ml.x - higher), old = fast_exp2(top - higher);
+                top = higher;
+                l = l * old + by * ml.y;
+                o *= old;
+                const int count = (w.parts - s0 + per_row - 1) / per_row < 64 ? (w.parts - s0 + per_row - 1) / per_row : 64;
+                const float* from = prm.part_o + ((int64_t)(w.slot + s0) * prm.slot_rows + i) * kHeadDim + 2 * lane;
+                const int64_t stride = (int64_t)per_row * prm.slot_rows * kHeadDim;
+                for (int s = 0; s < count; s += 8) {
+                    f32x2_t x[8];
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const f32x2_t*>(from + (s + u < count ? s + u : s) * stride);
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const float weight = s + u < count ? lane_value(by, s + u) : 0.0f;
+                        o.x = __builtin_fmaf(x[u].x, weight, o.x);
+                        o.y = __builtin_fmaf(x[u].y, weight, o.y);
+                    }
+                }
             }
-            const int count = parts - s0 < 64 ? parts - s0 : 64;
-            for (int s = 0; s < count; ++s) {
-                const f32x2_t x = *reinterpret_cast<const f32x2_t*>(prm.part_o + ((first_slot + s0 + s) * prm.slot_rows + i) * kHeadDim + 2 * lane);
-                o += x * lane_value(by, s);
+            l = wave_sum(l);
+        }
+        if (per_row > 1) {
+            __syncthreads();      // the last unit's are read
+            sums[wave][lane] = o;
+            if (lane == 0) tops[wave] = f32x2_t{top, l};
+            __syncthreads();
+            if (mine == 0) {
+                float m = top;
+                for (int u = 1; u < per_row; ++u) m = fmaxf(m, tops[wave + u].x);
+                const float own = fast_exp2(top - m);
+                o *= own;
+                l *= own;
+                top = m;
+                for (int u = 1; u < per_row; ++u) {
+                    const f32x2_t ml = tops[wave + u], x = sums[wave + u][lane];
+                    const float by = fast_exp2(ml.x - m);
+                    l += by * ml.y;
+                    o += x * by;
+                }
             }
         }
-        l = wave_sum(l);
+        if (!on || mine != 0) continue;
         const int t = (int)((unsigned)row / (unsigned)prm.group);
-        const int64_t q_row = (int64_t)(w.s.first + t) * prm.n_q_heads + head * prm.group + (row - t * prm.group);
+        const int64_t q_row = (int64_t)(w.first + t) * prm.n_q_heads + w.head * prm.group + (row - t * prm.group);
         const float inv = l > 0.0f ? 1.0f / l : 0.0f;
         reinterpret_cast<uint32_t*>(prm.out + q_row * kHeadDim)[lane] = cvt_bf16(o.x * inv, o.y * inv);
         if (prm.lse && lane == 0) prm.lse[q_row] = l > 0.0f ? (top + __builtin_amdgcn_logf(l)) * kLn2 : kNegInf;
@@ -336,7 +420,7 @@ hipError_t launch_prefill(const PrefillParams& prm, hipStream_t stream) {
     const long grid = prefill_grid(prm.total_q, prm.batch, prm.group, prm.n_kv_heads);
     hipError_t e = launch(prefill_kernel, dim3((unsigned)grid), 64 * kWaves, stream, prm);
     if (e != hipSuccess) return e;
-    return launch(prefill_merge_kernel, dim3(kPrefillShares, kMergeSplit), 256, stream, prm);
+    return launch(prefill_merge_kernel, dim3(kMergeGroups), 64 * kMergeWaves, stream, prm);
 }
 
 }  // namespace xattn

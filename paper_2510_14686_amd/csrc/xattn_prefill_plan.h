@@ -22,7 +22,7 @@ constexpr int kPrefillRows = 128;
 constexpr int kPrefillKeys = 64;
 constexpr int kPrefillShares = 512;              // two workgroups per compute unit
 constexpr int kPrefillSlots = 2 * kPrefillShares;
-constexpr int kPrefillMinBlocks = 2;
+constexpr int kPrefillMinBlocks = 8;
 
 // New tokens [first, first + q) of the packed rows, clamped to those that there are.
 struct PrefillSeq {

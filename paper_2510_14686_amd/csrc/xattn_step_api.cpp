@@ -50,13 +50,14 @@ int check_prefill(const char* who, int batch, int total_q, int n_q_heads, int n_
 
 struct PrefillLayout {
     int slot_rows;
-    size_t o_off, total;
+    size_t ml_off, o_off, total;
 };
 PrefillLayout prefill_layout(int total_q, int group) {
     PrefillLayout w;
     w.slot_rows = prefill_slot_rows(total_q, group);
     const size_t rows = (size_t)kPrefillSlots * w.slot_rows;
-    w.o_off = align_up(rows * 2 * sizeof(float), 256);
+    w.ml_off = align_up(kPrefillTableBytes, 256);
+    w.o_off = w.ml_off + align_up(rows * 2 * sizeof(float), 256);
     w.total = w.o_off + rows * kHeadDim * sizeof(float);
     return w;
 }
@@ -115,12 +116,13 @@ int xattn_prefill(const void* q, const void* const* k_ptrs, const void* const* v
     prm.slot_rows = w.slot_rows;
     struct Call {
         PrefillParams* prm;
-        size_t o_off;
+        size_t ml_off, o_off;
         hipStream_t stream;
-    } call = {&prm, w.o_off, static_cast<hipStream_t>(stream)};
+    } call = {&prm, w.ml_off, w.o_off, static_cast<hipStream_t>(stream)};
     return with_workspace(who, w.total, stream, [](void* context, char* ws) {
         const Call& c = *static_cast<Call*>(context);
-        c.prm->part_ml = reinterpret_cast<float*>(ws);
+        c.prm->table = reinterpret_cast<int32_t*>(ws);
+        c.prm->part_ml = reinterpret_cast<float*>(ws + c.ml_off);
         c.prm->part_o = reinterpret_cast<float*>(ws + c.o_off);
         const hipError_t e = launch_prefill(*c.prm, c.stream);
         return e == hipSuccess ? (int)XATTN_OK : fail_hip(e, "kernel launch");

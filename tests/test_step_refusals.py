@@ -70,7 +70,7 @@ def test_workspace_sizes():
     for batch, total, hq, hkv in ((1, 1, 8, 8), (4, 55, 8, 2), (16, 40000, 32, 8)):
         rows = min(128, total * hq // hkv)
         ml = (1024 * rows * 8 + 255) // 256 * 256
-        assert xa.xattn_prefill_workspace_bytes(batch, total, hq, hkv) == ml + 1024 * rows * 512
+        assert xa.xattn_prefill_workspace_bytes(batch, total, hq, hkv) == 16640 + ml + 1024 * rows * 512
     assert xa.xbeam_logprobs_workspace_bytes(4096, 131072, 5) == 256      # a workgroup per row
     for rows, vocab, k in ((1, 131072, 20), (3, 100003, 512), (200, 100003, 0)):
         n = xa.xbeam_logprobs_workspace_bytes(rows, vocab, k)
