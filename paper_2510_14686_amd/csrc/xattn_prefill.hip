@@ -9,6 +9,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "xattn_device.h"
 #include "xattn_launch.h"
 #include "xattn_prefill.h"
@@ -23,6 +25,8 @@ constexpr int kWaves = 4;
 constexpr int kWaveRows = kPrefillRows / kWaves;      // 32: the MFMA's columns
 constexpr int kBlockBytes = kPrefillKeys * kRowBytes; // 16 KiB of K, or of V
 constexpr float kLowest = -3.0e38f;                   // reference of a row that has seen no key
+constexpr int kHalfBytes = kBlockBytes / 2;
+constexpr int kAhead = 4;                             // steps of the next scores ahead of the row maxima
 constexpr float kSlackLog2 = 8.0f;                    // how far a row's maximum may exceed its reference
 
 // ------------------------------------------------------------------------------------------------ a workgroup's work
@@ -145,18 +149,23 @@ __device__ __forceinline__ int* split_count(const PrefillParams& prm) { return p
 __device__ __forceinline__ SplitTile* split_tiles(const PrefillParams& prm) { return reinterpret_cast<SplitTile*>(prm.table + 8); }
 
 // ------------------------------------------------------------------------------------------------ blocks
-// Block at key0 of K or V: 1024 chunks of 16 bytes, four per thread, thread t chunk t % 16 of rows t / 16 + 16 i.  The descriptor
-// ends with the sequence, so rows behind it (which an xTensor range need not have mapped) read as zero, and begins with the
-// block, so a sequence may be larger than 32-bit offsets reach.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t block_rsrc(const char* head, int key0, int kv, int row_bytes) {
+// Block at key0 of K or V, loaded into LDS without passing through registers: a wave's load fills 1024 consecutive bytes, four rows,
+// lane l the l-th 16 bytes.  The descriptor ends with the sequence, so rows behind it (which an xTensor range need not have mapped) read
+// as zero, and begins with the block, so a sequence may be larger than 32-bit offsets reach.
+__device__ __forceinline__ u32x4_t block_rsrc(const char* head, int key0, int kv, int row_bytes) {
     const int keys = kv - key0 < kPrefillKeys ? kv - key0 : kPrefillKeys;
-    return make_rsrc(head + (int64_t)key0 * row_bytes, keys > 0 ? (uint32_t)((keys - 1) * row_bytes + kRowBytes) : 0u);
+    const uint64_t base = (uint64_t)(uintptr_t)(head + (int64_t)key0 * row_bytes);
+    return u32x4_t{(uint32_t)base, (uint32_t)(base >> 32) & 0xffffu, keys > 0 ? (uint32_t)((keys - 1) * row_bytes + kRowBytes) : 0u, 0x00020000u};
 }
+// The loads are assembly because the compiler would wait for all of them ahead of every read of LDS; wait_loads() and the barrier
+// behind it are what makes a block visible.  m0 is the address in LDS; a wait state goes between its write and the load.
+__device__ __forceinline__ void load_lds(u32x4_t rsrc, uint32_t lds_addr, uint32_t voff, uint32_t soff) {
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "{m0}"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
+}
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // In LDS a row is 256 bytes.  K: chunk c of row r sits at c ^ (r & 15), so that the 16 rows that 16 lanes read a chunk
 // of are in different banks; V: 64-byte piece x of row r at x ^ (r & 3), for the four rows of a transposing read.
-__device__ __forceinline__ int k_off(int row, int chunk) { return row * kRowBytes + ((chunk ^ (row & 15)) << 4); }
-__device__ __forceinline__ int v_off(int row, int chunk) { return row * kRowBytes + ((chunk ^ ((row & 3) << 2)) << 4); }
 
 // S^T = K Q^T by 32x32x16 MFMA: lane (hh, n) = (lane / 32, lane % 32) gives chunk 8 hh .. of key row n and of query row n, and
 // has, of query row n, the keys at rows 8 (i / 4) + 4 hh + i % 4 in accumulator i.  Row x of the operand is key tile_row(x) of the
@@ -165,16 +174,16 @@ __device__ __forceinline__ int v_off(int row, int chunk) { return row * kRowByte
 __device__ __forceinline__ int tile_row(int x) { return (x & ~12) | ((x & 4) << 1) | ((x & 8) >> 1); }
 
 __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams prm) {
-    __shared__ __attribute__((aligned(16))) char lds[2 * 2 * kBlockBytes];
+    __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * kBlockBytes];      // K, K, V, V
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
     const int n = lane & 31, hh = lane >> 5;
-    const int head = blockIdx.x % (unsigned)prm.n_kv_heads;
-    const PrefillWork w = find_work(prm, (int)(blockIdx.x / (unsigned)prm.n_kv_heads), lane);
+    const int head = uniform((int)(blockIdx.x % (unsigned)prm.n_kv_heads));
+    const PrefillWork w = find_work(prm, uniform((int)(blockIdx.x / (unsigned)prm.n_kv_heads)), lane);
     if (blockIdx.x == 0 && tid == 0) *split_count(prm) = w.splits * prm.n_kv_heads;
     if (!w.found) return;
     // Later tiles see more keys: first.
-    const int tile = w.s.tiles - 1 - w.index / w.parts, part = w.index % w.parts;
-    const int part_blocks = prefill_part_blocks(w.s.blocks, w.parts), blocks = prefill_tile_blocks(w.s, tile, prm.group);
+    const int tile = uniform(w.s.tiles - 1 - w.index / w.parts), part = uniform(w.index % w.parts);
+    const int part_blocks = uniform(prefill_part_blocks(w.s.blocks, w.parts)), blocks = uniform(prefill_tile_blocks(w.s, tile, prm.group));
     const int blk0 = part * part_blocks, blk1 = blk0 + part_blocks < blocks ? blk0 + part_blocks : blocks;
     if (part > 0 && blk0 >= blk1) return;
     const bool whole = blocks <= part_blocks;
@@ -184,8 +193,9 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
             SplitTile{w.s.first, w.s.q, tile, head, first_slot, whole ? 1 : (blocks + part_blocks - 1) / part_blocks, {0, 0}};
 
     const int row_bytes = prm.n_kv_heads * kRowBytes;
-    const char* const k_head = w.k + head * kRowBytes;
-    const char* const v_head = w.v + head * kRowBytes;
+    const char* const k_head = static_cast<const char*>(uniform(static_cast<const void*>(w.k + head * kRowBytes)));
+    const char* const v_head = static_cast<const char*>(uniform(static_cast<const void*>(w.v + head * kRowBytes)));
+    const int kv = uniform(w.s.kv);
 
     // This lane's query row.
     const int rows = w.s.q * prm.group, wave_row = tile * kPrefillRows + wave * kWaveRows, row = wave_row + n;
@@ -210,26 +220,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     for (int c = 0; c < 4; ++c) o[c] = f32x16_t{};
     float m = kLowest, l = 0.0f;
 
-    // Loads of a block, and their way into LDS.
-    const int load_row = tid >> 4, load_chunk = tid & 15;
-    uint32_t load_off[4];
+    // This wave's loads of a block: rows 16 wave + 4 i + lane / 16, i < 4, of K and of V.
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    const int load_row = 16 * wave + (lane >> 4), load_chunk = lane & 15;
+    uint32_t k_load[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load_off[i] = (uint32_t)((load_row + 16 * i) * row_bytes + load_chunk * 16);
-    u32x4_t stage[8];
-    auto load_block = [&](int blk) {
-        const __amdgpu_buffer_rsrc_t rk = block_rsrc(k_head, blk * kPrefillKeys, w.s.kv, row_bytes);
-        const __amdgpu_buffer_rsrc_t rv = block_rsrc(v_head, blk * kPrefillKeys, w.s.kv, row_bytes);
+    for (int i = 0; i < 4; ++i) k_load[i] = (uint32_t)((load_row + 4 * i) * row_bytes + ((load_chunk ^ ((load_row + 4 * i) & 15)) << 4));
+    const uint32_t v_load = (uint32_t)(load_row * row_bytes + ((load_chunk ^ ((load_row & 3) << 2)) << 4));
+    // K of block j is in buffer j & 1.  V comes and goes by half blocks of 32 keys, half g = 2 j + h of the sequence to place g & 3; a load
+    // is of two, from an odd one on.
+    auto load_k = [&](int blk) {
+        const u32x4_t rsrc = block_rsrc(k_head, blk * kPrefillKeys, kv, row_bytes);
+        const uint32_t to = lds0 + (blk & 1) * kBlockBytes + wave * 4096;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) stage[i] = __builtin_amdgcn_raw_buffer_load_b128(rk, (int)load_off[i], 0, 0);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) stage[4 + i] = __builtin_amdgcn_raw_buffer_load_b128(rv, (int)load_off[i], 0, 0);
+        for (int i = 0; i < 4; ++i) load_lds(rsrc, to + i * 1024, k_load[i], 0u);
     };
-    auto store_block = [&](char* to) {
+    auto load_v = [&](int half) {
+        const u32x4_t rsrc = block_rsrc(v_head, half * 32, kv, row_bytes);
+        const uint32_t to = lds0 + 2 * kBlockBytes + ((half + (wave >> 1)) & 3) * kHalfBytes + (wave & 1) * 4096;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            *reinterpret_cast<u32x4_t*>(to + k_off(load_row, load_chunk) + 16 * i * kRowBytes) = stage[i];
-            *reinterpret_cast<u32x4_t*>(to + kBlockBytes + v_off(load_row, load_chunk) + 16 * i * kRowBytes) = stage[4 + i];
-        }
+        for (int i = 0; i < 4; ++i) load_lds(rsrc, to + i * 1024, v_load, (uint32_t)(4 * i * row_bytes));
+    };
+    auto load_v_first = [&](int half) {      // one half, by the first two waves
+        const u32x4_t rsrc = block_rsrc(v_head, half * 32, kv, row_bytes);
+        const uint32_t to = lds0 + 2 * kBlockBytes + (half & 3) * kHalfBytes + wave * 4096;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_lds(rsrc, to + i * 1024, v_load, (uint32_t)(4 * i * row_bytes));
     };
 
     // Where the lane reads.  Keys: row tile_row(n), chunk 2 s + hh.  Values, by transposing reads: a 16-lane group's lane 4 j + i
@@ -238,74 +254,88 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     const int k_row = tile_row(n);
     const int k_read = k_row * kRowBytes + ((hh ^ (k_row & 15)) << 4);
     const int piece = 4 * ((lane >> 4) & 1) + (lane & 3), v_row = 8 * hh + ((lane >> 2) & 3);
-    const int v_read = kBlockBytes + v_row * kRowBytes + ((v_row & 3) << 6) + (4 * (piece & 1) + (piece >> 1)) * 8;
+    const int v_read = 2 * kBlockBytes + v_row * kRowBytes + ((v_row & 3) << 6) + (4 * (piece & 1) + (piece >> 1)) * 8;
+    int v_turn[3];      // from there to columns 32 c .. 32 c + 31, c > 0
+#pragma unroll
+    for (int c = 1; c < 4; ++c) v_turn[c - 1] = (v_read ^ (c << 6)) - v_read;
 
-    if (blk0 < blk1) {
-        load_block(blk0);
-        store_block(lds);
-    }
-    __syncthreads();
-    for (int blk = blk0; blk < blk1; ++blk) {
-        const char* const cur = lds + ((blk - blk0) & 1) * (2 * kBlockBytes);
-        char* const next = lds + ((blk - blk0 + 1) & 1) * (2 * kBlockBytes);
-        const bool more = blk + 1 < blk1;
-        if (more) load_block(blk + 1);
-        const int key0 = blk * kPrefillKeys;
-        if (key0 < lim_last) {
-            f32x16_t s[2];
+    // Half g's scores.
+    auto score_step = [&](f32x16_t& s, int g, int i) {      // step i of 8
+        const char* const from = lds + ((g >> 1) & 1) * kBlockBytes + (g & 1) * kHalfBytes;
+        const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(from + (k_read ^ (i << 5)));
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qop[i], i == 0 ? f32x16_t{} : s, 0, 0, 0);
+    };
+    // They become weights, while the matrix pipe works on the scores of the half after it, and add its values up.
+    auto half = [&](f32x16_t& s, f32x16_t& next, int g) {
+        const int key0 = 32 * g;
+        if (key0 + 32 > lim_first) {
 #pragma unroll
-            for (int kt = 0; kt < 2; ++kt) {
-                s[kt] = f32x16_t{};
+            for (int i = 0; i < 16; ++i) s[i] = key0 + 16 * (i >> 3) + 8 * hh + (i & 7) < lim ? s[i] : kNegInf;
+        }
 #pragma unroll
-                for (int st = 0; st < 8; ++st) {
-                    const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(cur + (k_read ^ (st << 5)) + kt * 32 * kRowBytes);
-                    s[kt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qop[st], s[kt], 0, 0, 0);
-                }
-            }
-            if (key0 + kPrefillKeys > lim_first) {
+        for (int i = 0; i < kAhead; ++i) score_step(next, g + 1, i);
+        float mx = s[0];
 #pragma unroll
-                for (int kt = 0; kt < 2; ++kt)
+        for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
+        float a, b;
+        swap32(mx, a, b);
+        mx = fmaxf(a, b) * prm.scale_log2;
+        // The reference moves only when a row exceeds it by 2^8: then a weight is 2^8 at most, which neither the sums nor
+        // bf16 mind, and most blocks need no rescaling of o.
+        if (__ballot(mx > m + kSlackLog2) != 0) {
+            const float to = fmaxf(m, mx), by = fast_exp2(m - to);
+            m = to;
+            l *= by;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        s[kt][i] = key0 + 32 * kt + 16 * (i >> 3) + 8 * hh + (i & 7) < lim ? s[kt][i] : kNegInf;
-            }
-            float mx = s[0][0];
+            for (int c = 0; c < 4; ++c) o[c] *= by;
+        }
 #pragma unroll
-            for (int i = 1; i < 32; ++i) mx = fmaxf(mx, s[i >> 4][i & 15]);
-            float a, b;
-            swap32(mx, a, b);
-            mx = fmaxf(a, b) * prm.scale_log2;
-            // The reference moves only when a row exceeds it by 2^8: then a weight is 2^8 at most, which neither the sums nor
-            // bf16 mind, and most blocks need no rescaling of o.
-            if (__ballot(mx > m + kSlackLog2) != 0) {
-                const float to = fmaxf(m, mx), by = fast_exp2(m - to);
-                m = to;
-                l *= by;
+        for (int i = kAhead; i < 8; ++i) score_step(next, g + 1, i);
+        float p[16];
 #pragma unroll
-                for (int c = 0; c < 4; ++c) o[c] *= by;
-            }
-            float p[32];
+        for (int i = 0; i < 16; ++i) {
+            p[i] = fast_exp2(__builtin_fmaf(s[i], prm.scale_log2, -m));
+            l += p[i];
+        }
+        const char* const from = lds + v_read + (g & 3) * kHalfBytes;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                p[i] = fast_exp2(__builtin_fmaf(s[i >> 4][i & 15], prm.scale_log2, -m));
-                l += p[i];
-            }
+        for (int st = 0; st < 2; ++st) {
+            const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{cvt_bf16(p[8 * st], p[8 * st + 1]), cvt_bf16(p[8 * st + 2], p[8 * st + 3]),
+                                                                     cvt_bf16(p[8 * st + 4], p[8 * st + 5]), cvt_bf16(p[8 * st + 6], p[8 * st + 7])});
 #pragma unroll
-            for (int st = 0; st < 4; ++st) {
-                const u32x4_t pw = {cvt_bf16(p[8 * st], p[8 * st + 1]), cvt_bf16(p[8 * st + 2], p[8 * st + 3]),
-                                    cvt_bf16(p[8 * st + 4], p[8 * st + 5]), cvt_bf16(p[8 * st + 6], p[8 * st + 7])};
-                const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, pw);
-#pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const char* const at = cur + (v_read ^ (c << 6)) + st * 16 * kRowBytes;
-                    const u32x2_t v0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)at));
-                    const u32x2_t v1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)(at + 4 * kRowBytes)));
-                    o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{v0.x, v0.y, v1.x, v1.y}), pb, o[c], 0, 0, 0);
-                }
+            for (int c = 0; c < 4; ++c) {
+                const char* const at = from + (c == 0 ? 0 : v_turn[c - 1]) + st * 16 * kRowBytes;
+                const u32x2_t v0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)at));
+                const u32x2_t v1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)(at + 4 * kRowBytes)));
+                o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{v0.x, v0.y, v1.x, v1.y}), pb, o[c], 0, 0, 0);
             }
         }
-        if (more) store_block(next);
+    };
+
+    // Round j: the weights of half 2 j beside the scores of half 2 j + 1, then the weights of that beside the scores of 2 j + 2 (behind the
+    // last one, of whatever the buffer holds: they are not used).  What the second half of the round and the first of the next one read is
+    // loaded meanwhile, block j + 1 of K and halves 2 j + 1 and 2 j + 2 of V, into buffers that were last read ahead of the barrier.  A wave
+    // whose rows see no more keys goes on with its share of the loads and the barriers.
+    if (blk0 < blk1) {
+        load_k(blk0);
+        if (wave < 2) load_v_first(2 * blk0);
+        wait_loads();
         __syncthreads();
+        if (blk0 + 1 < blk1) load_k(blk0 + 1);
+        load_v(2 * blk0 + 1);
+        f32x16_t s0, s1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) score_step(s0, 2 * blk0, i);
+        for (int j = blk0; j < blk1; ++j) {
+            if (64 * j < lim_last) half(s0, s1, 2 * j);
+            wait_loads();
+            __syncthreads();
+            if (j + 1 < blk1) {
+                if (j + 2 < blk1) load_k(j + 2);
+                load_v(2 * j + 3);
+            }
+            if (64 * j + 32 < lim_last) half(s1, s0, 2 * j + 1);
+        }
     }
 
     float la, lb;
