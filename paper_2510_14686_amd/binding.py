@@ -325,15 +325,27 @@ def xattn_prefill_workspace_bytes(batch: int, total_q: int, n_q_heads: int, n_kv
     return n
 
 
+_sections_arrays = {}      # the C arrays of the sections that calls have named so far, by their values
+
+
+def _sections_array(sections):
+    key = tuple(sections)
+    array = _sections_arrays.get(key)
+    if array is None:
+        array = (ctypes.c_int * len(key))(*key)
+        if len(_sections_arrays) < 64:
+            _sections_arrays[key] = array
+    return array
+
+
 def xattn_rope_kvcache(q, k_new, v_new, q_stride: int, k_stride: int, v_stride: int, pos, inv_freq, sections, flags: int, k_ptrs, v_ptrs,
                        q_starts, kv_lens, batch: int, total_q: int, n_q_heads: int, n_kv_heads: int, head_dim: int, q_out, stream=None) -> None:
     """Enqueue the rotation of q and k_new and the append of k_new and v_new; see include/xattn.h.  Strides in values; sections: a
     sequence of integers, one per axis."""
     if stream is not None and not isinstance(stream, int):
         stream = int(stream.cuda_stream)
-    n_axes = len(sections)
     status = (_lib or load_library()).xattn_rope_kvcache(_ptr(q), _ptr(k_new), _ptr(v_new), q_stride, k_stride, v_stride, _ptr(pos), _ptr(inv_freq),
-                                                         (ctypes.c_int * n_axes)(*sections), n_axes, flags, _ptr(k_ptrs), _ptr(v_ptrs),
+                                                         _sections_array(sections), len(sections), flags, _ptr(k_ptrs), _ptr(v_ptrs),
                                                          _ptr(q_starts), _ptr(kv_lens), batch, total_q, n_q_heads, n_kv_heads, head_dim,
                                                          _ptr(q_out), stream)
     if status < 0:

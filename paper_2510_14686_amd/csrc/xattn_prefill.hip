@@ -159,8 +159,11 @@ __device__ __forceinline__ u32x4_t block_rsrc(const char* head, int key0, int kv
 }
 // The loads are assembly because the compiler would wait for all of them ahead of every read of LDS; wait_loads() and the barrier
 // behind it are what makes a block visible.  m0 is the address in LDS; a wait state goes between its write and the load.
+// kOnce: non-temporal.
+template <bool kOnce>
 __device__ __forceinline__ void load_lds(u32x4_t rsrc, uint32_t lds_addr, uint32_t voff, uint32_t soff) {
-    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "{m0}"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
+    if constexpr (kOnce) asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen nt lds" : : "{m0}"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
+    else asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" : : "{m0}"(lds_addr), "v"(voff), "s"(rsrc), "s"(soff) : "memory");
 }
 __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -229,23 +232,24 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     const uint32_t v_load = (uint32_t)(load_row * row_bytes + ((load_chunk ^ ((load_row & 3) << 2)) << 4));
     // K of block j is in buffer j & 1.  V comes and goes by half blocks of 32 keys, half g = 2 j + h of the sequence to place g & 3; a load
     // is of two, from an odd one on.
-    auto load_k = [&](int blk) {
+    // What a single tile reads, as of a decoding sequence, is read once: non-temporal (64 of 4096 keys, one new token, 8 KV heads 196 ->
+    // 173 us); K and V of several tiles are to stay in the L2.
+    const bool once = uniform(w.s.tiles) == 1;
+    auto load_k_as = [&](auto as, int blk) {
         const u32x4_t rsrc = block_rsrc(k_head, blk * kPrefillKeys, kv, row_bytes);
         const uint32_t to = lds0 + (blk & 1) * kBlockBytes + wave * 4096;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_lds(rsrc, to + i * 1024, k_load[i], 0u);
+        for (int i = 0; i < 4; ++i) load_lds<decltype(as)::value>(rsrc, to + i * 1024, k_load[i], 0u);
     };
-    auto load_v = [&](int half) {
+    auto load_v_as = [&](auto as, int half, int place) {
         const u32x4_t rsrc = block_rsrc(v_head, half * 32, kv, row_bytes);
-        const uint32_t to = lds0 + 2 * kBlockBytes + ((half + (wave >> 1)) & 3) * kHalfBytes + (wave & 1) * 4096;
+        const uint32_t to = lds0 + 2 * kBlockBytes + (place & 3) * kHalfBytes + (wave & 1) * 4096;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) load_lds(rsrc, to + i * 1024, v_load, (uint32_t)(4 * i * row_bytes));
+        for (int i = 0; i < 4; ++i) load_lds<decltype(as)::value>(rsrc, to + i * 1024, v_load, (uint32_t)(4 * i * row_bytes));
     };
-    auto load_v_first = [&](int half) {      // one half, by the first two waves
-        const u32x4_t rsrc = block_rsrc(v_head, half * 32, kv, row_bytes);
-        const uint32_t to = lds0 + 2 * kBlockBytes + (half & 3) * kHalfBytes + wave * 4096;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load_lds(rsrc, to + i * 1024, v_load, (uint32_t)(4 * i * row_bytes));
+    auto load_next = [&](auto as, int blk) {      // block blk of K, and halves 2 blk - 1 and 2 blk of V
+        if (blk < blk1) load_k_as(as, blk);
+        load_v_as(as, 2 * blk - 1, 2 * blk - 1 + (wave >> 1));
     };
 
     // Where the lane reads.  Keys: row tile_row(n), chunk 2 s + hh.  Values, by transposing reads: a 16-lane group's lane 4 j + i
@@ -259,21 +263,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
 #pragma unroll
     for (int c = 1; c < 4; ++c) v_turn[c - 1] = (v_read ^ (c << 6)) - v_read;
 
-    // Half g's scores.
-    auto score_step = [&](f32x16_t& s, int g, int i) {      // step i of 8
-        const char* const from = lds + ((g >> 1) & 1) * kBlockBytes + (g & 1) * kHalfBytes;
-        const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(from + (k_read ^ (i << 5)));
+    // Half g's scores, in eight steps.
+    auto key_operand = [&](int g, int i) {
+        return *reinterpret_cast<const bf16x8_t*>(lds + ((g >> 1) & 1) * kBlockBytes + (g & 1) * kHalfBytes + (k_read ^ (i << 5)));
+    };
+    auto score_step = [&](f32x16_t& s, const bf16x8_t& a, int i) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qop[i], i == 0 ? f32x16_t{} : s, 0, 0, 0);
+    };
+    // Columns 32 c .. 32 c + 31 of keys 16 st .. 16 st + 15 of a half.
+    auto value_operand = [&](int g, int st, int c) {
+        const char* const at = lds + v_read + (g & 3) * kHalfBytes + (c == 0 ? 0 : v_turn[c - 1]) + st * 16 * kRowBytes;
+        const u32x2_t v0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)at));
+        const u32x2_t v1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)(at + 4 * kRowBytes)));
+        return __builtin_bit_cast(bf16x8_t, u32x4_t{v0.x, v0.y, v1.x, v1.y});
     };
     // They become weights, while the matrix pipe works on the scores of the half after it, and add its values up.
     auto half = [&](f32x16_t& s, f32x16_t& next, int g) {
+        bf16x8_t ka[8], va[2][4];
         const int key0 = 32 * g;
         if (key0 + 32 > lim_first) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = key0 + 16 * (i >> 3) + 8 * hh + (i & 7) < lim ? s[i] : kNegInf;
         }
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i) score_step(next, g + 1, i);
+        for (int i = 0; i < 8; ++i) ka[i] = key_operand(g + 1, i);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) score_step(next, ka[i], i);
         float mx = s[0];
 #pragma unroll
         for (int i = 1; i < 16; ++i) mx = fmaxf(mx, s[i]);
@@ -290,25 +305,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
             for (int c = 0; c < 4; ++c) o[c] *= by;
         }
 #pragma unroll
-        for (int i = kAhead; i < 8; ++i) score_step(next, g + 1, i);
+        for (int c = 0; c < 4; ++c) va[0][c] = value_operand(g, 0, c);
+#pragma unroll
+        for (int i = kAhead; i < 8; ++i) score_step(next, ka[i], i);
         float p[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             p[i] = fast_exp2(__builtin_fmaf(s[i], prm.scale_log2, -m));
             l += p[i];
         }
-        const char* const from = lds + v_read + (g & 3) * kHalfBytes;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) va[1][c] = value_operand(g, 1, c);
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{cvt_bf16(p[8 * st], p[8 * st + 1]), cvt_bf16(p[8 * st + 2], p[8 * st + 3]),
                                                                      cvt_bf16(p[8 * st + 4], p[8 * st + 5]), cvt_bf16(p[8 * st + 6], p[8 * st + 7])});
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const char* const at = from + (c == 0 ? 0 : v_turn[c - 1]) + st * 16 * kRowBytes;
-                const u32x2_t v0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)at));
-                const u32x2_t v1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)(at + 4 * kRowBytes)));
-                o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, u32x4_t{v0.x, v0.y, v1.x, v1.y}), pb, o[c], 0, 0, 0);
-            }
+            for (int c = 0; c < 4; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[st][c], pb, o[c], 0, 0, 0);
         }
     };
 
@@ -317,22 +330,21 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     // loaded meanwhile, block j + 1 of K and halves 2 j + 1 and 2 j + 2 of V, into buffers that were last read ahead of the barrier.  A wave
     // whose rows see no more keys goes on with its share of the loads and the barriers.
     if (blk0 < blk1) {
-        load_k(blk0);
-        if (wave < 2) load_v_first(2 * blk0);
+        load_k_as(std::false_type(), blk0);
+        if (wave < 2) load_v_as(std::false_type(), 2 * blk0, 2 * blk0);      // one half, by two waves
         wait_loads();
         __syncthreads();
-        if (blk0 + 1 < blk1) load_k(blk0 + 1);
-        load_v(2 * blk0 + 1);
+        load_next(std::false_type(), blk0 + 1);
         f32x16_t s0, s1;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) score_step(s0, 2 * blk0, i);
+        for (int i = 0; i < 8; ++i) score_step(s0, key_operand(2 * blk0, i), i);
         for (int j = blk0; j < blk1; ++j) {
             if (64 * j < lim_last) half(s0, s1, 2 * j);
             wait_loads();
             __syncthreads();
             if (j + 1 < blk1) {
-                if (j + 2 < blk1) load_k(j + 2);
-                load_v(2 * j + 3);
+                if (once) load_next(std::true_type(), j + 2);
+                else load_next(std::false_type(), j + 2);
             }
             if (64 * j + 32 < lim_last) half(s1, s0, 2 * j + 1);
         }
@@ -380,8 +392,8 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prefill_merge_kernel(Prefill
     while (per_row < kMergeWaves && tiles * (kPrefillRows / kMergeWaves) * per_row * 2 <= kMergeGroups) per_row *= 2;
     const int rows_at_once = kMergeWaves / per_row, steps = kPrefillRows / rows_at_once;
     for (int unit = blockIdx.x; unit < tiles * steps; unit += kMergeGroups) {
-        const SplitTile w = split_tiles(prm)[unit / steps];
-        const int i = unit % steps * rows_at_once + wave / per_row, row = w.tile * kPrefillRows + i, mine = wave % per_row;
+        const SplitTile w = split_tiles(prm)[unit % tiles];      // the tiles' first rows first: some tiles have no others
+        const int i = unit / tiles * rows_at_once + wave / per_row, row = w.tile * kPrefillRows + i, mine = wave % per_row;
         // (Of bounds in q_starts that do not ascend, an entry may not have been written: nothing outside the buffers then.)
         const bool known = w.parts > 1 && w.parts <= kPrefillSlots && (unsigned)w.slot <= (unsigned)(kPrefillSlots - w.parts) && (unsigned)w.head < (unsigned)prm.n_kv_heads &&
                            (unsigned)w.first <= (unsigned)prm.total_q && (unsigned)w.q <= (unsigned)(prm.total_q - w.first) && (unsigned)w.tile < 1u << 24;

@@ -119,7 +119,17 @@ __device__ __forceinline__ uint64_t cut_list(uint64_t* list, int count, int k, i
     return least;
 }
 
-// The key of the r-th largest of the lanes' values, or a little less (16 bits of it).
+// The r-th largest of the lanes' keys, of which each has two, or a little less (16 bits of it).
+__device__ __forceinline__ uint32_t nth_of_two(uint32_t one, uint32_t other, int r) {
+    uint32_t at = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; --bit) {
+        const uint32_t trial = at | 1u << bit;
+        if (__builtin_popcountll(__ballot(one >= trial)) + __builtin_popcountll(__ballot(other >= trial)) >= r) at = trial;
+    }
+    return at;
+}
+// The key of the r-th largest of the lanes' values, or a little less.
 __device__ __forceinline__ uint32_t nth_key(float x, int r) {
     if (r <= 4) {      // a few times the largest of those left; lanes that share it count together
         float best = wave_max(x);
@@ -130,14 +140,7 @@ __device__ __forceinline__ uint32_t nth_key(float x, int r) {
         }
         return order_key(best);
     }
-    const uint32_t key = order_key(x);
-    uint32_t at = 0;
-#pragma unroll
-    for (int bit = 31; bit >= 16; --bit) {
-        const uint32_t trial = at | 1u << bit;
-        if (__builtin_popcountll(__ballot(key >= trial)) >= r) at = trial;
-    }
-    return at;
+    return nth_of_two(order_key(x), 0u, r);
 }
 
 // What the workgroup's threads need of LDS to pick and order candidates.
@@ -213,9 +216,12 @@ __device__ __forceinline__ uint64_t keep_best(uint64_t (&mine)[kRegs], int k, ui
     return least;
 }
 
-// How many candidates are kept where k are asked for: what ranking or the bitonic network below takes.
+// How many candidates are ranked by counting the better ones, a thread each; of more a bitonic network is faster.
 template <int kWaves>
-__device__ __forceinline__ int most_kept(int k) { return kWaves < kRowWaves || k <= 128 ? 128 : kMaxTopK; }
+constexpr int kRanked = kWaves == kRowWaves ? 256 : 128;
+// How many candidates are kept where k are asked for.
+template <int kWaves>
+__device__ __forceinline__ int most_kept(int k) { return k <= kRanked<kWaves> ? kRanked<kWaves> : kMaxTopK; }
 
 template <int kRegs>
 __device__ __forceinline__ int count_all(const uint64_t (&mine)[kRegs]) {      // the wave's
@@ -265,7 +271,7 @@ __device__ __forceinline__ int gather_best(uint64_t (&mine)[kRegs], int kept, in
         if (mine[i] != 0) ws.list[at + before(here)] = mine[i];
         at += __builtin_popcountll(here);
     }
-    if (n <= 128 && tid < 8) ws.list[n + tid] = 0;      // ranks are counted eight at a time
+    if (n <= kRanked<kWaves> && tid < 8) ws.list[n + tid] = 0;      // ranks are counted eight at a time
     __syncthreads();
     return n;
 }
@@ -300,8 +306,8 @@ template <int kWaves, int kRegs, typename Put>
 __device__ __forceinline__ int rank_candidates(uint64_t (&mine)[kRegs], int k, uint64_t least, int bits, PickSpace& ws, int tid, Put put) {
     const int lane = tid & 63, wave = uniform(tid >> 6);
     const int n = gather_best<kWaves, kRegs>(mine, count_all(mine), k, least, bits, ws, tid);
-    if (n <= 128) {
-        if (tid < 128 && wave * 64 < n) {
+    if (n <= kRanked<kWaves>) {
+        if (wave * 64 < n) {
             const uint64_t x = tid < n ? ws.list[tid] : 0;
             const int rank = rank_of(x, ws.list, n);
             if (tid < n) put(rank, x);
@@ -498,7 +504,18 @@ __global__ __launch_bounds__(64 * kWaves, 4) void logprobs_kernel(LogprobsParams
     }
 
     // The lanes' sums, then the waves'.
-    if constexpr (kTop) raise();
+    if constexpr (kList) raise();
+    if constexpr (kCap == kAtOnce) {
+        // All values are here: twice as many maxima, each of half of a lane's, put tau nearer to the k-th value.
+        float one = x[0], other = x[kVals / 2];
+#pragma unroll
+        for (int i = 1; i < kVals / 2; ++i) {
+            one = fmaxf(one, x[i]);
+            other = fmaxf(other, x[kVals / 2 + i]);
+        }
+        const uint32_t mine = wave >= with_values ? 0u : per_wave <= 4 ? nth_key(top, per_wave) : nth_of_two(order_key(one), order_key(other), per_wave);
+        if (lane == 0) taus[wave] = mine;
+    }
     const float wave_top = wave_max(top);
     {
         const float m = fmaxf(wave_top, -kFar);
