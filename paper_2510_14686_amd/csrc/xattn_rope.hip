@@ -57,6 +57,35 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams prm) {
     __shared__ int known[kTokens];              // whether a sequence has it
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
     const int token0 = blockIdx.x * kTokens;
+    const int lanes = kLanes ? kLanes : prm.head_dim / 16, slots = prm.n_q_heads + 2 * prm.n_kv_heads;
+    const int items = slots * lanes * kTokens, turned = prm.frequencies / 8;
+    // An item: 16 values of a head of a row, in two pieces.
+    struct Item {
+        int tk, head, c, at0, at1;
+        bool is_q, is_k, turn;
+        u32x4_t x, y;
+    };
+    auto fetch = [&](int item) {
+        Item r;
+        r.c = (int)((unsigned)item % (unsigned)lanes);
+        const int slot = (int)((unsigned)item / (unsigned)lanes % (unsigned)slots);
+        r.tk = (int)((unsigned)item / (unsigned)lanes / (unsigned)slots);
+        r.is_q = slot < prm.n_q_heads;
+        r.is_k = !r.is_q && slot < prm.n_q_heads + prm.n_kv_heads;
+        r.head = r.is_q ? slot : r.is_k ? slot - prm.n_q_heads : slot - prm.n_q_heads - prm.n_kv_heads;
+        r.turn = r.c < turned && (r.is_q || r.is_k);
+        const bool apart = r.turn && !prm.pairs;
+        r.at0 = apart ? 8 * r.c : 16 * r.c;
+        r.at1 = apart ? prm.frequencies + 8 * r.c : 16 * r.c + 8;
+        const int64_t row = token0 + r.tk < prm.total_q ? token0 + r.tk : prm.total_q - 1;
+        const uint16_t* const from =
+            (r.is_q ? prm.q + row * prm.q_stride : r.is_k ? prm.k + row * prm.k_stride : prm.v + row * prm.v_stride) + r.head * prm.head_dim;
+        r.x = *reinterpret_cast<const u32x4_t*>(from + r.at0);
+        r.y = *reinterpret_cast<const u32x4_t*>(from + r.at1);
+        return r;
+    };
+    // The first one is on its way while the rows' sequences are looked for.
+    Item next = fetch((int)threadIdx.x < items ? (int)threadIdx.x : 0);
     if (wave < kTokens) {
         const int row = token0 + wave;
         int start = 0, end = 0;
@@ -80,28 +109,20 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams prm) {
     }
     __syncthreads();
 
-    const int lanes = kLanes ? kLanes : prm.head_dim / 16, slots = prm.n_q_heads + 2 * prm.n_kv_heads;
-    const int items = slots * lanes * kTokens, turned = prm.frequencies / 8;
     for (int item = threadIdx.x; item < items; item += kRopeThreads) {
-        const int c = (int)((unsigned)item % (unsigned)lanes), slot = (int)((unsigned)item / (unsigned)lanes % (unsigned)slots);
-        const int tk = (int)((unsigned)item / (unsigned)lanes / (unsigned)slots);
-        if (!known[tk]) continue;
-        const int64_t row = token0 + tk;
-        const bool is_q = slot < prm.n_q_heads, is_k = !is_q && slot < prm.n_q_heads + prm.n_kv_heads;
-        const int head = is_q ? slot : is_k ? slot - prm.n_q_heads : slot - prm.n_q_heads - prm.n_kv_heads;
-        const uint16_t* from = (is_q ? prm.q + row * prm.q_stride : is_k ? prm.k + row * prm.k_stride : prm.v + row * prm.v_stride) + head * prm.head_dim;
-        uint16_t* to = is_q ? prm.q_out + row * prm.n_q_heads * prm.head_dim : rows[tk][is_k ? 0 : 1];
+        Item it = next;
+        if (item + kRopeThreads < items) next = fetch(item + kRopeThreads);
+        if (!known[it.tk]) continue;
+        uint16_t* to = it.is_q ? prm.q_out + (int64_t)(token0 + it.tk) * prm.n_q_heads * prm.head_dim : rows[it.tk][it.is_k ? 0 : 1];
         if (to == nullptr) continue;
-        to += head * prm.head_dim;
-        const bool turn = c < turned && (is_q || is_k), apart = turn && !prm.pairs;
-        const int at0 = apart ? 8 * c : 16 * c, at1 = apart ? prm.frequencies + 8 * c : 16 * c + 8;
-        u32x4_t x = *reinterpret_cast<const u32x4_t*>(from + at0), y = *reinterpret_cast<const u32x4_t*>(from + at1);
-        if (turn) {
+        to += it.head * prm.head_dim;
+        u32x4_t &x = it.x, &y = it.y;
+        if (it.turn) {
             float co[8], si[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                co[i] = cosines[tk][8 * c + i];
-                si[i] = sines[tk][8 * c + i];
+                co[i] = cosines[it.tk][8 * it.c + i];
+                si[i] = sines[it.tk][8 * it.c + i];
             }
             if (prm.pairs) {
 #pragma unroll
@@ -119,8 +140,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams prm) {
                 }
             }
         }
-        *reinterpret_cast<u32x4_t*>(to + at0) = x;
-        *reinterpret_cast<u32x4_t*>(to + at1) = y;
+        *reinterpret_cast<u32x4_t*>(to + it.at0) = x;
+        *reinterpret_cast<u32x4_t*>(to + it.at1) = y;
     }
 }
 
