@@ -25,12 +25,34 @@ struct LogprobsParams {
     float* entropy;
     char* workspace;                 // of several parts per row
 };
+
+constexpr int kRowWaves = 8;                     // waves of a workgroup; kFewWaves where rows are short
+constexpr int kFewWaves = 2;
+constexpr int kStep = 512;                       // values that a wave loads as one row of 8 (or two of 4) per lane
+constexpr int kLoads = 2;                        // steps of a wave in a round
+constexpr int kAtOnceSize = kRowWaves * kLoads * kStep;      // values that a workgroup's registers hold
+constexpr int kParts = 256;                      // workgroups that rows are cut for
+constexpr int kFewRounds = 6;                    // of a row that is not cut
+constexpr int kMostMerged = 8192;                // candidates that the merge of a row's parts holds
+
 // How a call's rows are cut.
 struct LogprobsCut {
-    int parts, part_size;            // parts of a row, and their logits (a multiple of 512 but for the last)
+    int parts, part_size;            // parts of a row, and their logits (a multiple of kStep but for the last)
     size_t workspace;                // bytes; 0 with one part
 };
-LogprobsCut logprobs_cut(int rows, int vocab, int top_k);
+// A round is kAtOnceSize values and takes a workgroup about 1 us, putting parts together 6 to 8 us (a second launch): rows of more
+// than kFewRounds rounds are cut where they are few.  1 / 128 rows of 40000, 20 alternatives 12.3 / 13.8 us whole (of kFewRounds = 3, cut,
+// 12.0 / 17.3); 1 / 128 of 60000 12.4 / 17.5 cut (15.3 / 16.3 whole).  kParts 512: 64 of 131072 19.6 -> 25.0.
+inline LogprobsCut logprobs_cut(int rows, int vocab, int top_k) {
+    const int at_once = (vocab + kAtOnceSize - 1) / kAtOnceSize;
+    int parts = kParts / rows < at_once ? kParts / rows : at_once;
+    if (top_k > 0 && parts > kMostMerged / top_k) parts = kMostMerged / top_k;
+    if (at_once <= kFewRounds) parts = 1;
+    if (parts <= 1) return LogprobsCut{1, vocab, 0};
+    const int steps = (vocab + kStep - 1) / kStep, size = (steps + parts - 1) / parts * kStep;
+    parts = (vocab + size - 1) / size;
+    return LogprobsCut{parts, size, parts > 1 ? (size_t)rows * parts * (16 + 8 * (size_t)top_k) : 0};
+}
 hipError_t launch_logprobs(const LogprobsParams& prm, const LogprobsCut& cut, hipStream_t stream);
 
 }  // namespace xattn

@@ -25,16 +25,8 @@
 namespace xattn {
 namespace {
 
-constexpr int kRowWaves = 8;                     // waves of a workgroup; kFewWaves where rows are short
-constexpr int kFewWaves = 2;
-constexpr int kStep = 512;                       // values that a wave loads as one row of 8 (or two of 4) per lane
-constexpr int kLoads = 2;                        // steps of a wave in a round
 constexpr int kVals = kLoads * kStep / 64;       // a lane's values in a round
-constexpr int kAtOnceSize = kRowWaves * kLoads * kStep;      // values that a workgroup's registers hold
 constexpr int kAtOnce = -1;
-constexpr int kParts = 256;                      // workgroups that rows are cut for
-constexpr int kFewRounds = 6;                    // of a row that is not cut
-constexpr int kMostMerged = 8192;                // candidates that the merge of a row's parts holds
 constexpr float kFar = 1e30f;                    // logits beyond are summed up in a second pass, whose differences do not overflow
 
 // Bits that order as the values do; NaN below everything (0), -0 as 0.
@@ -674,18 +666,6 @@ hipError_t launch_type(const LogprobsParams& prm, const LogprobsCut& cut, hipStr
 }
 
 }  // namespace
-
-LogprobsCut logprobs_cut(int rows, int vocab, int top_k) {
-    // A round is kAtOnceSize values and takes a workgroup about 1 us, putting parts together 6 to 8 us (a second launch).
-    const int at_once = (vocab + kAtOnceSize - 1) / kAtOnceSize;
-    int parts = kParts / rows < at_once ? kParts / rows : at_once;
-    if (top_k > 0 && parts > kMostMerged / top_k) parts = kMostMerged / top_k;
-    if (at_once <= kFewRounds) parts = 1;
-    if (parts <= 1) return LogprobsCut{1, vocab, 0};
-    const int steps = (vocab + kStep - 1) / kStep, size = (steps + parts - 1) / parts * kStep;
-    parts = (vocab + size - 1) / size;
-    return LogprobsCut{parts, size, parts > 1 ? (size_t)rows * parts * (16 + 8 * (size_t)top_k) : 0};
-}
 
 hipError_t launch_logprobs(const LogprobsParams& prm, const LogprobsCut& cut, hipStream_t stream) {
     switch (prm.dtype) {

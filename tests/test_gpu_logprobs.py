@@ -99,7 +99,7 @@ def test_temperatures(scale):
 
 
 @pytest.mark.parametrize("k", [1, 20, 64, 65, 512])
-@pytest.mark.parametrize("rows,vocab", [(2, 40000), (600, 6000)])
+@pytest.mark.parametrize("rows,vocab", [(2, 40000), (3, 60001), (300, 20000), (600, 6000), (530, 1999)])
 def test_orders_that_fill_the_lists(rows, vocab, k):
     """Rows that ascend, descend, are all equal, hold few different values, or have their best at the end."""
     up = torch.linspace(-3, 3, vocab, device="cuda").repeat(rows, 1)
@@ -114,7 +114,7 @@ def test_orders_that_fill_the_lists(rows, vocab, k):
 @pytest.mark.parametrize("dtype", list(KINDS), ids=str)
 def test_forbidden_tokens(dtype):
     for mask in (-math.inf, torch.finfo(dtype).min):
-        for rows, vocab in ((3, 30000), (520, 700)):
+        for rows, vocab in ((3, 30000), (2, 70000), (520, 700)):
             logits = normal(rows, vocab, dtype, seed=4).contiguous()
             logits[:, torch.rand(vocab, device="cuda") < 0.9] = mask
             logits[1] = mask
@@ -127,7 +127,7 @@ def test_forbidden_tokens(dtype):
                 assert not torch.isnan(r["lse"]).any() and not torch.isnan(r["entropy"]).any()
 
 
-@pytest.mark.parametrize("rows,vocab", [(2, 30000), (520, 700)])
+@pytest.mark.parametrize("rows,vocab", [(2, 30000), (2, 70000), (9, 8000), (520, 700)])
 def test_rows_of_nothing_but_forbidden_tokens(rows, vocab):
     logits = normal(rows, vocab, seed=5).contiguous()
     logits[1] = -math.inf
@@ -144,7 +144,7 @@ def test_rows_of_nothing_but_forbidden_tokens(rows, vocab):
     assert bool(((r["top_lp"][1] + math.log(vocab)).abs() <= (vocab / 512 + 400) * U).all())
 
 
-@pytest.mark.parametrize("rows,vocab", [(2, 30000), (520, 700)])
+@pytest.mark.parametrize("rows,vocab", [(2, 30000), (2, 70000), (9, 8000), (520, 700)])
 def test_values_that_are_no_numbers(rows, vocab):
     logits = normal(rows, vocab, seed=6).contiguous()
     clean = run(logits, 4)
@@ -176,9 +176,10 @@ def test_zeros_of_both_signs_are_equal():
     assert r["top_tok"][0].tolist() == list(range(100, 150))
 
 
-def test_large_values():
+@pytest.mark.parametrize("vocab", [5000, 9000, 60000])
+def test_large_values(vocab):
     for big in (1e31, 3e38, -1e31):
-        logits = normal(2, 9000, seed=7).contiguous()
+        logits = normal(2, vocab, seed=7).contiguous()
         logits[1] = -3e38
         logits[1, 4000:4002] = big
         r = run(logits, 3)
@@ -186,6 +187,26 @@ def test_large_values():
         assert r["top_tok"][1].tolist() == [4000, 4001, 0]
         assert abs(r["entropy"][1].item() - math.log(2)) < 1e-5 and r["lse"][1].item() == np.float32(big)
         assert bool(((r["top_lp"][1, :2] + math.log(2)).abs() < 1e-5).all())
+
+
+@pytest.mark.parametrize("k", [1, 7, 100, 512])
+def test_last_part_of_a_few_values(k):
+    """122883 logits are cut into 16 parts, the last of three values, fewer than a load takes."""
+    logits = normal(1, 122883, torch.bfloat16, seed=16).contiguous()
+    check(logits, k, run(logits, k))
+    logits[0, -3:] = 30.0
+    check(logits, k, run(logits, k))
+    logits[0, -3:] = -math.inf
+    check(logits, k, run(logits, k))
+
+
+def test_short_rows_of_few_values():
+    """Fewer logits than a load takes, also where most are forbidden."""
+    for vocab in range(1, 9):
+        for dtype in KINDS:
+            logits = normal(40, vocab, dtype, seed=vocab).contiguous()
+            logits[::3, 0] = -math.inf if vocab > 1 else 0.0
+            check(logits, vocab, run(logits, vocab))
 
 
 def test_tokens_outside():
