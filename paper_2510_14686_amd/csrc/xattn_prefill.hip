@@ -230,26 +230,27 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
 #pragma unroll
     for (int i = 0; i < 4; ++i) k_load[i] = (uint32_t)((load_row + 4 * i) * row_bytes + ((load_chunk ^ ((load_row + 4 * i) & 15)) << 4));
     const uint32_t v_load = (uint32_t)(load_row * row_bytes + ((load_chunk ^ ((load_row & 3) << 2)) << 4));
-    // K of block j is in buffer j & 1.  V comes and goes by half blocks of 32 keys, half g = 2 j + h of the sequence to place g & 3; a load
+    // K of the part's block j is in buffer j & 1.  V comes and goes by half blocks of 32 keys, half g = 2 j + h to place g & 3; a load
     // is of two, from an odd one on.
     // What a single tile reads, as of a decoding sequence, is read once: non-temporal (64 of 4096 keys, one new token, 8 KV heads 196 ->
     // 173 us); K and V of several tiles are to stay in the L2.
     const bool once = uniform(w.s.tiles) == 1;
-    auto load_k_as = [&](auto as, int blk) {
-        const u32x4_t rsrc = block_rsrc(k_head, blk * kPrefillKeys, kv, row_bytes);
-        const uint32_t to = lds0 + (blk & 1) * kBlockBytes + wave * 4096;
+    const int n_blocks = blk1 - blk0, first_key = blk0 * kPrefillKeys;
+    auto load_k_as = [&](auto as, int j) {
+        const u32x4_t rsrc = block_rsrc(k_head, (blk0 + j) * kPrefillKeys, kv, row_bytes);
+        const uint32_t to = lds0 + (j & 1) * kBlockBytes + wave * 4096;
 #pragma unroll
         for (int i = 0; i < 4; ++i) load_lds<decltype(as)::value>(rsrc, to + i * 1024, k_load[i], 0u);
     };
-    auto load_v_as = [&](auto as, int half, int place) {
-        const u32x4_t rsrc = block_rsrc(v_head, half * 32, kv, row_bytes);
+    auto load_v_as = [&](auto as, int g, int place) {
+        const u32x4_t rsrc = block_rsrc(v_head, blk0 * kPrefillKeys + g * 32, kv, row_bytes);
         const uint32_t to = lds0 + 2 * kBlockBytes + (place & 3) * kHalfBytes + (wave & 1) * 4096;
 #pragma unroll
         for (int i = 0; i < 4; ++i) load_lds<decltype(as)::value>(rsrc, to + i * 1024, v_load, (uint32_t)(4 * i * row_bytes));
     };
-    auto load_next = [&](auto as, int blk) {      // block blk of K, and halves 2 blk - 1 and 2 blk of V
-        if (blk < blk1) load_k_as(as, blk);
-        load_v_as(as, 2 * blk - 1, 2 * blk - 1 + (wave >> 1));
+    auto load_next = [&](auto as, int j) {      // block j of K, and halves 2 j - 1 and 2 j of V
+        if (j < n_blocks) load_k_as(as, j);
+        load_v_as(as, 2 * j - 1, 2 * j - 1 + (wave >> 1));
     };
 
     // Where the lane reads.  Keys: row tile_row(n), chunk 2 s + hh.  Values, by transposing reads: a 16-lane group's lane 4 j + i
@@ -259,34 +260,38 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     const int k_read = k_row * kRowBytes + ((hh ^ (k_row & 15)) << 4);
     const int piece = 4 * ((lane >> 4) & 1) + (lane & 3), v_row = 8 * hh + ((lane >> 2) & 3);
     const int v_read = 2 * kBlockBytes + v_row * kRowBytes + ((v_row & 3) << 6) + (4 * (piece & 1) + (piece >> 1)) * 8;
-    int v_turn[3];      // from there to columns 32 c .. 32 c + 31, c > 0
+    // (The addresses of all reads of a half, but for what the half adds to them, a constant in each of the four forms of it.)
+    const char *k_at[8], *v_at[4];
 #pragma unroll
-    for (int c = 1; c < 4; ++c) v_turn[c - 1] = (v_read ^ (c << 6)) - v_read;
+    for (int i = 0; i < 8; ++i) k_at[i] = lds + (k_read ^ (i << 5));
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v_at[c] = lds + (v_read ^ (c << 6));
 
-    // Half g's scores, in eight steps.
-    auto key_operand = [&](int g, int i) {
-        return *reinterpret_cast<const bf16x8_t*>(lds + ((g >> 1) & 1) * kBlockBytes + (g & 1) * kHalfBytes + (k_read ^ (i << 5)));
+    // The scores of half kG (of 4 in LDS), in eight steps.
+    auto key_operand = [&](auto half, int i) {
+        constexpr int kG = decltype(half)::value & 3;
+        return *reinterpret_cast<const bf16x8_t*>(k_at[i] + (kG >> 1) * kBlockBytes + (kG & 1) * kHalfBytes);
     };
     auto score_step = [&](f32x16_t& s, const bf16x8_t& a, int i) {
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, qop[i], i == 0 ? f32x16_t{} : s, 0, 0, 0);
     };
     // Columns 32 c .. 32 c + 31 of keys 16 st .. 16 st + 15 of a half.
-    auto value_operand = [&](int g, int st, int c) {
-        const char* const at = lds + v_read + (g & 3) * kHalfBytes + (c == 0 ? 0 : v_turn[c - 1]) + st * 16 * kRowBytes;
+    auto value_operand = [&](auto half, int st, int c) {
+        const char* const at = v_at[c] + decltype(half)::value * kHalfBytes + st * 16 * kRowBytes;
         const u32x2_t v0 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)at));
         const u32x2_t v1 = __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4v_t*)(at + 4 * kRowBytes)));
         return __builtin_bit_cast(bf16x8_t, u32x4_t{v0.x, v0.y, v1.x, v1.y});
     };
-    // They become weights, while the matrix pipe works on the scores of the half after it, and add its values up.
-    auto half = [&](f32x16_t& s, f32x16_t& next, int g) {
+    // The scores of the half from key0 on become weights, while the matrix pipe works on those of the half after it, and add its values up.
+    auto half = [&](auto which, f32x16_t& s, f32x16_t& next, int key0) {
+        constexpr int kG = decltype(which)::value;
         bf16x8_t ka[8], va[2][4];
-        const int key0 = 32 * g;
         if (key0 + 32 > lim_first) {
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[i] = key0 + 16 * (i >> 3) + 8 * hh + (i & 7) < lim ? s[i] : kNegInf;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ka[i] = key_operand(g + 1, i);
+        for (int i = 0; i < 8; ++i) ka[i] = key_operand(std::integral_constant<int, kG + 1>(), i);
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) score_step(next, ka[i], i);
         float mx = s[0];
@@ -305,7 +310,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
             for (int c = 0; c < 4; ++c) o[c] *= by;
         }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) va[0][c] = value_operand(g, 0, c);
+        for (int c = 0; c < 4; ++c) va[0][c] = value_operand(which, 0, c);
 #pragma unroll
         for (int i = kAhead; i < 8; ++i) score_step(next, ka[i], i);
         float p[16];
@@ -315,7 +320,7 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
             l += p[i];
         }
 #pragma unroll
-        for (int c = 0; c < 4; ++c) va[1][c] = value_operand(g, 1, c);
+        for (int c = 0; c < 4; ++c) va[1][c] = value_operand(which, 1, c);
 #pragma unroll
         for (int st = 0; st < 2; ++st) {
             const bf16x8_t pb = __builtin_bit_cast(bf16x8_t, u32x4_t{cvt_bf16(p[8 * st], p[8 * st + 1]), cvt_bf16(p[8 * st + 2], p[8 * st + 3]),
@@ -329,24 +334,32 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
     // last one, of whatever the buffer holds: they are not used).  What the second half of the round and the first of the next one read is
     // loaded meanwhile, block j + 1 of K and halves 2 j + 1 and 2 j + 2 of V, into buffers that were last read ahead of the barrier.  A wave
     // whose rows see no more keys goes on with its share of the loads and the barriers.
-    if (blk0 < blk1) {
-        load_k_as(std::false_type(), blk0);
-        if (wave < 2) load_v_as(std::false_type(), 2 * blk0, 2 * blk0);      // one half, by two waves
+    if (n_blocks > 0) {
+        load_k_as(std::false_type(), 0);
+        if (wave < 2) load_v_as(std::false_type(), 0, 0);      // one half, by two waves
         wait_loads();
         __syncthreads();
-        load_next(std::false_type(), blk0 + 1);
+        load_next(std::false_type(), 1);
         f32x16_t s0, s1;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) score_step(s0, key_operand(2 * blk0, i), i);
-        for (int j = blk0; j < blk1; ++j) {
-            if (64 * j < lim_last) half(s0, s1, 2 * j);
+        for (int i = 0; i < 8; ++i) score_step(s0, key_operand(std::integral_constant<int, 0>(), i), i);
+        auto round = [&](auto odd, int j) {
+            constexpr int kG = 2 * decltype(odd)::value;
+            const int key0 = first_key + j * kPrefillKeys;
+            if (key0 < lim_last) half(std::integral_constant<int, kG>(), s0, s1, key0);
             wait_loads();
             __syncthreads();
-            if (j + 1 < blk1) {
+            if (j + 1 < n_blocks) {
                 if (once) load_next(std::true_type(), j + 2);
                 else load_next(std::false_type(), j + 2);
             }
-            if (64 * j + 32 < lim_last) half(s1, s0, 2 * j + 1);
+            if (key0 + 32 < lim_last) half(std::integral_constant<int, kG + 1>(), s1, s0, key0 + 32);
+        };
+        for (int j = 0;;) {
+            round(std::integral_constant<int, 0>(), j);
+            if (++j >= n_blocks) break;
+            round(std::integral_constant<int, 1>(), j);
+            if (++j >= n_blocks) break;
         }
     }
 
