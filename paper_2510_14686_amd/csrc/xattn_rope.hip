@@ -3,7 +3,10 @@
 //
 //   (x, y) -> (x cos a - y sin a, y cos a + x sin a),  a = pos[axis of i][row] * inv_freq[i],  for every pair i of every head
 //
-// Bound by memory: a row is read once and written once.  A workgroup takes kTokens rows: a wave per row finds the row's sequence
+// Bound by memory: a row is read once and written once.  Two prompts of 4096 to 8191, 32 / 8 heads, 299 MB: 51 us, 5.9 TB/s, where a copy
+// of 1 GiB makes 5.2; 256 sequences' single tokens, 40 / 8 heads: 6 us, of which the angles and two dependent loads are most.  (Loads
+// and stores past the caches: 2048 tokens 11.7 -> 14 us; what is written is read next.)
+//   A workgroup takes kTokens rows: a wave per row finds the row's sequence
 // and works the angles out, into LDS, once for all heads; then all threads move 32 bytes at a time.
 // Angles are reduced to a fraction of a turn in double: a far position times a frequency has more digits than a float (position
 // 4000000 would be off by 0.2 rad).
@@ -154,7 +157,13 @@ hipError_t launch_rope(const RopeParams& prm, hipStream_t stream) {
         return prm.head_dim == 128 ? launch(rope_kernel<kTokens, 8>, grid, kRopeThreads, stream, prm)
                                    : launch(rope_kernel<kTokens, 0>, grid, kRopeThreads, stream, prm);
     };
-    return prm.total_q < 1024 ? with(std::integral_constant<int, 1>()) : with(std::integral_constant<int, 4>());
+    // A workgroup of few short rows has threads without work, one of more rows than its threads need moves them in more turns of its loop.
+    // Of 1 / 2 / 4 rows each, in us: 256 rows of 40 / 8 heads 5.8 / 6.5 / 8.4, 2000 rows 13.1 / 12.2 / 13.2, 16384 rows 86.4 / 89.0 / 95.1; 16384
+    // of 64 / 8 heads 120 / 127 / 135, of 16 / 8 47.2 / 41.7 / 43.5; 65536 of 8 / 1 139 / 90 / 69.
+    const int items = (prm.n_q_heads + 2 * prm.n_kv_heads) * (prm.head_dim / 16);      // of a row
+    return prm.total_q < 1024 || items > 2 * kRopeThreads ? with(std::integral_constant<int, 1>())
+           : items > kRopeThreads / 2                     ? with(std::integral_constant<int, 2>())
+                                                          : with(std::integral_constant<int, 4>());
 }
 
 }  // namespace xattn

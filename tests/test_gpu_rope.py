@@ -127,6 +127,14 @@ def test_heads_and_many_rows(hq, hkv):
     b.check()
 
 
+@pytest.mark.parametrize("d,hq,hkv", [(16, 40, 4), (80, 6, 3), (80, 24, 4), (96, 64, 16), (256, 6, 2), (256, 30, 10)])
+def test_rows_of_many_sizes(d, hq, hkv):
+    """Rows with little and with much to move, enough of them that several may share a workgroup, the last ones alone in theirs."""
+    b = Batch([(1, 1 + i % 9) for i in range(100)] + [(1001, 1300), (2, 2)], hq, hkv, d, [8 * (d // 32), 8 * (d // 16 - d // 32)], seed=d + hq)
+    b.call()
+    b.check()
+
+
 def test_batches():
     for batch in (64, 65, 1000, 4096):
         b = Batch([((i * 7) % 4, (i * 7) % 4 + i % 5) for i in range(batch)], 2, 1, 128, [64], extra=5, seed=batch)
