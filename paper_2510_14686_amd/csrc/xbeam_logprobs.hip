@@ -2,7 +2,9 @@
 //
 //   x = scale * logit;  s = sum exp(x - m), t = sum (x - m) exp(x - m);  lse = m + ln s;  lp = x - lse;  H = ln s - t / s
 //
-// Bound by memory: a row is read once.  Every lane keeps m (its own maximum), s and t of its values, moved on when m moves, and the
+// Long rows are bound by memory, and by about ten instructions per value beside it: 4096 rows of 131072 bf16 logits, 5 alternatives, 191 us, 5.6
+// TB/s.  Short rows with many alternatives are bound by picking and ordering them: 1024 rows of 8192 fp32, 512 alternatives, 25 us, of which
+// the sums take 9, what may be one of the best 6, picking 6 and ordering 4.  A row is read once.  Every lane keeps m (its own maximum), s and t of its values, moved on when m moves, and the
 // lanes' are put together at the end.
 //
 // Alternatives: a lane's maximum is there anyway, and if in each of some waves ceil(k / 8) lanes have a maximum of tau or more, and
@@ -135,19 +137,38 @@ __device__ __forceinline__ uint32_t nth_key(float x, int r) {
     return nth_of_two(order_key(x), 0u, r);
 }
 
+// A thread's candidates: a bit of `on` for each that counts.
+template <int kRegs> struct Candidates {
+    static constexpr int kCount = kRegs;
+    uint64_t c[kRegs];
+    uint32_t on;
+    __device__ __forceinline__ uint32_t key(int i) const { return (uint32_t)(c[i] >> 32); }
+    __device__ __forceinline__ uint32_t place(int i) const { return (uint32_t)c[i]; }
+};
+// The same of values whose places follow from where their chunks are: half the registers.
+template <int kRegs, int kChunk> struct Values {
+    static constexpr int kCount = kRegs;
+    uint32_t keys[kRegs];
+    int from[kRegs / kChunk];
+    uint32_t on;
+    __device__ __forceinline__ uint32_t key(int i) const { return keys[i]; }
+    __device__ __forceinline__ uint32_t place(int i) const { return ~(uint32_t)(from[i / kChunk] + i % kChunk); }
+};
+template <typename Set> __device__ __forceinline__ uint64_t get(const Set& set, int i) { return (uint64_t)set.key(i) << 32 | set.place(i); }
+
 // What the workgroup's threads need of LDS to pick and order candidates.
 struct PickSpace {
     uint32_t bins[3][256];       // one counts, one is clear for the next round, one may still be read
-    int counts[kRowWaves];
+    int counts[kMostWaves];
     uint64_t list[kMaxTopK + 8];
 };
 
-// Leaves the k best of the threads' candidates (more than k of them; 0: none) and zeroes the others: their keys eight bits at a time
+// Leaves the k best of the threads' candidates (more than k of them) on, and no others: their keys eight bits at a time
 // from the top, each round counting the candidates that agree with the k-th so far by their next eight bits; then, where several share the
 // k-th's key, their places likewise.  low: a key that none is below; bits: of the largest difference from it.  Returns the least that is left.
 // Called by all threads.
-template <int kWaves, int kRegs>
-__device__ __forceinline__ uint64_t keep_best(uint64_t (&mine)[kRegs], int k, uint32_t low, int bits, PickSpace& ws, int tid) {
+template <int kWaves, typename Set>
+__device__ __forceinline__ uint64_t keep_best(Set& mine, int k, uint32_t low, int bits, PickSpace& ws, int tid) {
     const int lane = tid & 63;
     int need = k, round = 0;
     for (int i = tid; i < 256; i += 64 * kWaves) ws.bins[0][i] = 0;
@@ -160,7 +181,7 @@ __device__ __forceinline__ uint64_t keep_best(uint64_t (&mine)[kRegs], int k, ui
             shift -= width;
             uint32_t* const bins = ws.bins[round % 3];
 #pragma unroll
-            for (int i = 0; i < kRegs; ++i) {
+            for (int i = 0; i < Set::kCount; ++i) {
                 const uint32_t d = digits(i) >> shift;
                 if (counts(i) && d >> width == prefix) atomicAdd(bins + (d & ((1u << width) - 1)), 1u);
             }
@@ -196,32 +217,25 @@ __device__ __forceinline__ uint64_t keep_best(uint64_t (&mine)[kRegs], int k, ui
         }
     };
     int shift = bits;
-    const uint32_t key = low + find([&](int i) { return (uint32_t)(mine[i] >> 32) - low; }, [&](int i) { return mine[i] != 0; }, shift);
+    const uint32_t key = low + find([&](int i) { return mine.key(i) - low; }, [&](int i) { return (mine.on >> i & 1) != 0; }, shift);
     uint64_t least = (uint64_t)key << 32;
     if (need > 0) {
         shift = 32;
-        least |= find([&](int i) { return (uint32_t)mine[i]; }, [&](int i) { return (uint32_t)(mine[i] >> 32) == key; }, shift);
+        least |= find([&](int i) { return mine.place(i); }, [&](int i) { return (mine.on >> i & 1) != 0 && mine.key(i) == key; }, shift);
     }
 #pragma unroll
-    for (int i = 0; i < kRegs; ++i) mine[i] = mine[i] >= least ? mine[i] : 0;
+    for (int i = 0; i < Set::kCount; ++i) mine.on &= get(mine, i) >= least ? ~0u : ~(1u << i);
     __syncthreads();
     return least;
 }
 
 // How many candidates are ranked by counting the better ones, a thread each; of more a bitonic network is faster.
 template <int kWaves>
-constexpr int kRanked = kWaves == kRowWaves ? 256 : 128;
+constexpr int kRanked = kWaves >= kRowWaves ? 256 : 128;
 // How many candidates are kept where k are asked for.
 template <int kWaves>
 __device__ __forceinline__ int most_kept(int k) { return k <= kRanked<kWaves> ? kRanked<kWaves> : kMaxTopK; }
 
-template <int kRegs>
-__device__ __forceinline__ int count_all(const uint64_t (&mine)[kRegs]) {      // the wave's
-    int n = 0;
-#pragma unroll
-    for (int i = 0; i < kRegs; ++i) n += __builtin_popcountll(__ballot(mine[i] != 0));
-    return n;
-}
 // How many of the list's n candidates are better; it goes on with up to 7 zeros.
 __device__ __forceinline__ int rank_of(uint64_t c, const uint64_t* list, int n) {
     int rank = 0;
@@ -235,16 +249,19 @@ __device__ __forceinline__ int rank_of(uint64_t c, const uint64_t* list, int n) 
     return rank;
 }
 
-// Puts the threads' candidates (0: none; `kept` of them in the wave), or the k best where they are more than most_kept(k), into ws.list, in no order, and returns
-// how many there are.  least: none is below, raised to the least of the k best; bits: of the largest difference of a key from that one's.  Called by all threads, which find the list ready.
-template <int kWaves, int kRegs>
-__device__ __forceinline__ int gather_best(uint64_t (&mine)[kRegs], int kept, int k, uint64_t& least, int bits, PickSpace& ws, int tid) {
+// Puts the threads' candidates, or the k best where they are more than most_kept(k), into ws.list, in no order, and returns how many
+// there are.  least: none is below, raised to the least of the k best; bits: of the largest difference of a key from that one's.  Called
+// by all threads, which find the list ready.
+template <int kWaves, typename Set>
+__device__ __forceinline__ int gather_best(Set& mine, int k, uint64_t& least, int bits, PickSpace& ws, int tid) {
     const int lane = tid & 63, wave = uniform(tid >> 6);
     int n = 0, at = 0;
     for (bool again = true;; again = false) {
-        if (lane == 0) ws.counts[wave] = kept;
+        const int own = __builtin_popcount(mine.on), upto = wave_incl_scan_i(own);
+        if (lane == 63) ws.counts[wave] = upto;
         __syncthreads();
-        n = at = 0;
+        n = 0;
+        at = upto - own;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) {
             at += i < wave ? ws.counts[i] : 0;
@@ -252,17 +269,11 @@ __device__ __forceinline__ int gather_best(uint64_t (&mine)[kRegs], int kept, in
         }
         n = uniform(n);
         if (!again || n <= most_kept<kWaves>(k)) break;
-        least = keep_best<kWaves, kRegs>(mine, k, (uint32_t)(least >> 32), bits, ws, tid);
-        kept = count_all(mine);
+        least = keep_best<kWaves>(mine, k, (uint32_t)(least >> 32), bits, ws, tid);
     }
-    at = uniform(at);
 #pragma unroll
-    for (int i = 0; i < kRegs; ++i) {
-        const unsigned long long here = __ballot(mine[i] != 0);
-        if (here == 0) continue;
-        if (mine[i] != 0) ws.list[at + before(here)] = mine[i];
-        at += __builtin_popcountll(here);
-    }
+    for (int i = 0; i < Set::kCount; ++i)
+        if (mine.on >> i & 1) ws.list[at++] = get(mine, i);
     if (n <= kRanked<kWaves> && tid < 8) ws.list[n + tid] = 0;      // ranks are counted eight at a time
     __syncthreads();
     return n;
@@ -294,10 +305,10 @@ __device__ __forceinline__ void sort_step(uint64_t& x, int lane, bool down) {
 
 // Calls put(rank, candidate) for every one of the threads' candidates, or for the best of them, k at least; returns how many
 // it was called for.  Called by all threads, which are done with ws.list.
-template <int kWaves, int kRegs, typename Put>
-__device__ __forceinline__ int rank_candidates(uint64_t (&mine)[kRegs], int k, uint64_t least, int bits, PickSpace& ws, int tid, Put put) {
+template <int kWaves, typename Set, typename Put>
+__device__ __forceinline__ int rank_candidates(Set& mine, int k, uint64_t least, int bits, PickSpace& ws, int tid, Put put) {
     const int lane = tid & 63, wave = uniform(tid >> 6);
-    const int n = gather_best<kWaves, kRegs>(mine, count_all(mine), k, least, bits, ws, tid);
+    const int n = gather_best<kWaves>(mine, k, least, bits, ws, tid);
     if (n <= kRanked<kWaves>) {
         if (wave * 64 < n) {
             const uint64_t x = tid < n ? ws.list[tid] : 0;
@@ -307,7 +318,7 @@ __device__ __forceinline__ int rank_candidates(uint64_t (&mine)[kRegs], int k, u
         return n;
     }
     // A bitonic network, a candidate per thread: steps within a wave by lane exchanges, the six others through LDS.
-    if constexpr (kWaves == kRowWaves) {
+    if constexpr (kWaves >= kRowWaves) {
         uint64_t x = tid < n ? ws.list[tid] : 0;
         sort_step<2>(x, lane, (tid & 2) == 0);
         sort_step<4>(x, lane, (tid & 4) == 0);
@@ -318,9 +329,9 @@ __device__ __forceinline__ int rank_candidates(uint64_t (&mine)[kRegs], int k, u
         for (int size = 128; size <= kMaxTopK; size <<= 1) {
             for (int j = size >> 1; j >= 64; j >>= 1) {
                 __syncthreads();
-                ws.list[tid] = x;
+                if (kWaves == kRowWaves || tid < kMaxTopK) ws.list[tid] = x;
                 __syncthreads();
-                const uint64_t y = ws.list[tid ^ j];
+                const uint64_t y = ws.list[(tid ^ j) & (kMaxTopK - 1)];
                 x = (x > y) == (((tid & size) == 0) == ((tid & j) == 0)) ? x : y;
             }
             sort_step<64>(x, lane, (tid & size) == 0);
@@ -366,10 +377,11 @@ __device__ __host__ __forceinline__ PartSpace part_space(char* ws, int rows, int
     return PartSpace{reinterpret_cast<float*>(ws), reinterpret_cast<uint64_t*>(ws + (size_t)rows * parts * 16)};
 }
 
-// A row, or one of its parts, per workgroup.  kCap: chunks that a wave's list holds; 0 without alternatives, kAtOnce for alternatives of
+// A row, or one of its parts, per workgroup.  Where values stay in registers, eight waves to a SIMD at the price of a few spilled
+// registers: 1024 rows of 8192, 512 alternatives 26.4 -> 25.2 us, 4096 rows, 20 alternatives 47.1 -> 44.1.  kCap: chunks that a wave's list holds; 0 without alternatives, kAtOnce for alternatives of
 // rows (or parts) of one round, whose values stay in registers.
 template <typename T, int kCap, int kWaves>
-__global__ __launch_bounds__(64 * kWaves, 4) void logprobs_kernel(LogprobsParams prm, int parts, int part_size) {
+__global__ __launch_bounds__(64 * kWaves, kCap == kAtOnce ? 8 : 4) void logprobs_kernel(LogprobsParams prm, int parts, int part_size) {
     constexpr bool kTop = kCap != 0, kList = kCap > 0;
     __shared__ uint64_t lists[kList ? kWaves * kCap : 1];
     __shared__ uint32_t taus[kWaves];
@@ -398,13 +410,13 @@ __global__ __launch_bounds__(64 * kWaves, 4) void logprobs_kernel(LogprobsParams
         if (lane == 0) __hip_atomic_store(taus + wave, mine, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
     };
     auto look = [&]() {
-        // (The last three bits, made the wave's, keep them apart.)
-        const uint32_t mine = lane < kWaves ? (__hip_atomic_load(taus + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) & ~7u) | (uint32_t)lane : 0u;
+        // (The last bits, made the wave's, keep them apart.)
+        const uint32_t mine = lane < kWaves ? (__hip_atomic_load(taus + lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) & ~(kWaves - 1u)) | (uint32_t)lane : 0u;
         int better = 0;
 #pragma unroll
         for (int i = 0; i < kWaves; ++i) better += (uint32_t)__builtin_amdgcn_readlane((int)mine, i) > mine;
         const unsigned long long at = __ballot(lane < kWaves && better == enough - 1);
-        const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)mine, __builtin_ctzll(at | 1ull << 63)) & ~7u;
+        const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)mine, __builtin_ctzll(at | 1ull << 63)) & ~(kWaves - 1u);
         tau = all > tau ? all : tau;
     };
     // A round: kLoads steps per wave, the waves side by side in each, so that a short row has values for all, and a wave's rounds come in
@@ -560,37 +572,49 @@ __global__ __launch_bounds__(64 * kWaves, 4) void logprobs_kernel(LogprobsParams
             else if (rank < k) to.candidates[(int64_t)blockIdx.x * k + rank] = c;
         };
         if constexpr (!kList) {
-            uint64_t value[kVals];
+            Values<kVals, kChunk> value;
+            value.on = 0;
 #pragma unroll
-            for (int i = 0; i < kVals; ++i) {
-                const int q = i / kChunk, from = tiny ? 0 : last + (int)(ahead[q] / (uint32_t)sizeof(T)), at = from + i % kChunk;
-                const uint32_t key = order_key(x[i]);
-                value[i] = key >= tau && nominal(0, q) < end && at >= nominal(0, q) && at < end ? candidate(key, at) : 0;
+            for (int q = 0; q < kChunks; ++q) {
+                const int from = tiny ? 0 : last + (int)(ahead[q] / (uint32_t)sizeof(T)), skip = nominal(0, q) - from, count = tiny ? end : kChunk;
+                value.from[q] = from;
+                uint32_t on = 0;
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) {
+                    value.keys[q * kChunk + i] = order_key(x[q * kChunk + i]);
+                    on |= value.keys[q * kChunk + i] >= tau ? 1u << i : 0u;
+                }
+                // (Values from `first` on count, and of a tiny row those that there are.)
+                on &= skip < count ? (1u << count) - (1u << skip) : 0u;
+                value.on |= on << (q * kChunk);
             }
-            const int n = rank_candidates<kWaves, kVals>(value, k, least, bits, ws, tid, put);
+            const int n = rank_candidates<kWaves>(value, k, least, bits, ws, tid, put);
             for (int i = n + tid; i < k; i += 64 * kWaves) put(i, 0);
             return;
         } else {
-            uint64_t mine[kCap / 64];
+            Candidates<kCap / 64> mine;
+            mine.on = 0;
 #pragma unroll
             for (int i = 0; i < kCap / 64; ++i) {
-                mine[i] = 64 * i + lane < count ? list[64 * i + lane] : 0;
-                if ((uint32_t)(mine[i] >> 32) < tau) mine[i] = 0;
+                mine.c[i] = 64 * i + lane < count ? list[64 * i + lane] : 0;
+                if (64 * i + lane < count && mine.key(i) >= tau) mine.on |= 1u << i;
             }
-            const int chunks = gather_best<kWaves, kCap / 64>(mine, count_all(mine), k, least, bits, ws, tid);
+            const int chunks = gather_best<kWaves>(mine, k, least, bits, ws, tid);
             least &= ~0xffffffffull;      // places of chunks are not places of values
             // The chunks' values, a chunk per thread.
             static_assert(64 * kRowWaves >= kMaxTopK, "a thread for every chunk");
             const int first = tid < chunks ? (int)~(uint32_t)ws.list[tid] : end, from = first < end - kChunk ? first : end - kChunk;
             Chunk<T> chunk;
             chunk.load(logits + from);
-            uint64_t value[kChunk];
+            Values<kChunk, kChunk> value;
+            value.from[0] = from;
+            value.on = 0;
 #pragma unroll
             for (int i = 0; i < kChunk; ++i) {
-                const uint64_t c = candidate(order_key(chunk.get(i)), from + i);
-                value[i] = from + i >= first && from + i < end && c >= least && c >> 32 != 0 ? c : 0;
+                value.keys[i] = order_key(chunk.get(i));
+                if (from + i >= first && from + i < end && value.keys[i] >= (uint32_t)(least >> 32) && value.keys[i] != 0) value.on |= 1u << i;
             }
-            const int n = rank_candidates<kWaves, kChunk>(value, k, least, bits, ws, tid, put);
+            const int n = rank_candidates<kWaves>(value, k, least, bits, ws, tid, put);
             for (int i = n + tid; i < k; i += 64 * kWaves) put(i, 0);
         }
     }
@@ -606,9 +630,9 @@ __global__ __launch_bounds__(64 * kRowWaves) void logprobs_merge_kernel(Logprobs
     const float* const sums = from.sums + (int64_t)row * parts * 4;
     const uint64_t* const candidates = from.candidates + (int64_t)row * parts * k;
     constexpr int kRegs = kMostMerged / (64 * kRowWaves);
-    uint64_t mine[kRegs];
+    Candidates<kRegs> mine;
 #pragma unroll
-    for (int i = 0; i < kRegs; ++i) mine[i] = i * 64 * kRowWaves + tid < parts * k ? candidates[i * 64 * kRowWaves + tid] : 0;
+    for (int i = 0; i < kRegs; ++i) mine.c[i] = i * 64 * kRowWaves + tid < parts * k ? candidates[i * 64 * kRowWaves + tid] : 0;
     // Every wave by itself, a part per lane.
     float top = kNegInf;
     uint64_t least = 1, best = 0;    // k candidates of one part are that good; the best one
@@ -638,10 +662,12 @@ __global__ __launch_bounds__(64 * kRowWaves) void logprobs_merge_kernel(Logprobs
         least = l > least ? l : least;
         best = b > best ? b : best;
     }
+    mine.on = 0;
 #pragma unroll
-    for (int i = 0; i < kRegs; ++i) mine[i] = mine[i] >= least ? mine[i] : 0;
+    for (int i = 0; i < kRegs; ++i)
+        if (mine.c[i] >= least) mine.on |= 1u << i;
     auto put = [&](int rank, uint64_t x) { write_candidate(prm, row, rank, x, r.m, log_s); };
-    const int n = rank_candidates<kRowWaves, kRegs>(mine, k, least, 32 - __builtin_clz((uint32_t)(best >> 32) - (uint32_t)(least >> 32) | 1), ws, tid, put);
+    const int n = rank_candidates<kRowWaves>(mine, k, least, 32 - __builtin_clz((uint32_t)(best >> 32) - (uint32_t)(least >> 32) | 1), ws, tid, put);
     for (int i = n + tid; i < k; i += 64 * kRowWaves) put(i, 0);
 }
 
@@ -654,13 +680,16 @@ hipError_t launch_type(const LogprobsParams& prm, const LogprobsCut& cut, hipStr
     };
     const std::integral_constant<int, kRowWaves> many;
     const std::integral_constant<int, kFewWaves> few;
+    const std::integral_constant<int, kMostWaves> most;
     const bool is_short = cut.parts == 1 && prm.vocab <= kFewWaves * kLoads * kStep, at_once = cut.part_size <= kAtOnceSize;
+    const bool wide = grid.x <= kParts && cut.part_size > kManyRounds * kAtOnceSize;
     hipError_t e;
-    if (prm.top_k == 0) e = is_short ? with(std::integral_constant<int, 0>(), few) : with(std::integral_constant<int, 0>(), many);
+    const std::integral_constant<int, 0> none;
+    if (prm.top_k == 0) e = is_short ? with(none, few) : wide ? with(none, most) : with(none, many);
     else if (is_short && prm.top_k <= 128) e = with(std::integral_constant<int, kAtOnce>(), few);
     else if (at_once) e = with(std::integral_constant<int, kAtOnce>(), many);
-    else if (prm.top_k <= 64) e = with(std::integral_constant<int, 256>(), many);
-    else e = with(std::integral_constant<int, 640>(), many);
+    else if (prm.top_k <= 64) e = wide ? with(std::integral_constant<int, 256>(), most) : with(std::integral_constant<int, 256>(), many);
+    else e = wide ? with(std::integral_constant<int, 640>(), most) : with(std::integral_constant<int, 640>(), many);
     if (e != hipSuccess || cut.parts == 1) return e;
     return launch(logprobs_merge_kernel<T>, dim3((unsigned)prm.rows), 64 * kRowWaves, stream, prm, cut.parts);
 }

@@ -168,6 +168,39 @@ def test_values_that_are_no_numbers(rows, vocab):
     assert r["top_tok"][1].tolist() == [8, 0, 1, 2] and math.isnan(r["lse"][1].item()) and bool(r["top_lp"][1].isnan().all())
 
 
+@pytest.mark.parametrize("k", [0, 1, 50, 64, 65, 300, 512])
+@pytest.mark.parametrize("rows,vocab,dtype", [(129, 82000, torch.bfloat16), (131, 100003, torch.float32), (256, 90001, torch.float16), (257, 82000, torch.bfloat16)])
+def test_long_rows_of_a_batch(rows, vocab, dtype, k):
+    """Of any order, with forbidden tokens, values that are no numbers, and rows of nothing but forbidden tokens."""
+    logits = normal(rows, vocab + 3, dtype, seed=k)[:, :vocab]
+    logits[3] = torch.linspace(-3, 3, vocab, device="cuda").to(dtype)
+    logits[4] = logits[3].flip(0)
+    logits[5] = 1.0
+    logits[6] = logits[6].round()
+    logits[7, -700:] += 40
+    logits[8, torch.rand(vocab, device="cuda") < 0.99] = -math.inf
+    logits[9] = -math.inf
+    logits[9, 5], logits[9, vocab - 1] = 1.0, 1.0
+    logits[10] = torch.finfo(dtype).min
+    logits[10, vocab - 2] = 0.0
+    r = run(logits, k)
+    if k:
+        r["tokens"][:] = r["top_tok"][:, 0]
+    r = run(logits, k, out=r)
+    keep = [i for i in range(rows) if k or i not in (8, 9)]      # (a token of probability 0 has no finite log-probability)
+    if not k:
+        r["token_lp"][8:10] = 0
+        r = {n: v if v is None else v[keep] for n, v in r.items()}
+    check(logits[keep], k, r)
+    logits[2] = -math.inf
+    logits[1, 11] = math.nan
+    again = run(logits, k)
+    torch.cuda.synchronize()
+    assert again["lse"][2].item() == -math.inf and math.isnan(again["lse"][1].item()) and math.isnan(again["entropy"][1].item())
+    if k:
+        assert again["top_tok"][2].tolist() == list(range(k)) and 11 not in again["top_tok"][1].tolist()
+
+
 def test_zeros_of_both_signs_are_equal():
     logits = torch.full((1, 5000), -1.0, device="cuda")
     logits[0, 100:200:2], logits[0, 101:200:2] = -0.0, 0.0
