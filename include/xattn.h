@@ -151,7 +151,7 @@ int xattn_mla_decode(const void* q, const void* const* c_ptrs, const int32_t* kv
  * kv_lens  DEVICE  int32[batch]; keys visible to the sequence's last new token (its K/V are already written).  Tokens without
  *                  visible keys (kv_len < q_len) get out = 0 and lse = -inf.
  * batch 1..4096; total_q 1..2^24, the rows that q, out and lse have; total_q * n_q_heads <= 2^30; head_dim 128; n_q_heads <=
- * 1024, a multiple of n_kv_heads.  Otherwise XATTN_EUNSUPPORTED.  scale finite.
+ * 1024, a multiple of n_kv_heads.  Otherwise XATTN_EUNSUPPORTED.  scale and scale * log2 e finite.
  * out      DEVICE  bf16 [total_q, n_q_heads, head_dim], 16-byte aligned, not overlapping the inputs;  lse DEVICE fp32 [total_q, n_q_heads] or NULL
  * Same stream, capture and ownership rules as xattn_decode, same workspace (of at least xattn_prefill_workspace_bytes).
  * Numerics: scores, maxima and sums in fp32; a softmax weight enters the value product as one bf16 (off by 2^-8 of it at most,

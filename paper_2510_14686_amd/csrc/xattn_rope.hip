@@ -94,7 +94,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_kernel(RopeParams prm) {
         int start = 0, end = 0;
         const int b = row < prm.total_q ? find_sequence(prm.q_starts, prm.batch, row, lane, start, end) : -1;
         if (b >= 0) {
-            const int at = prm.kv_lens[b] - (end - row);
+            const int len = prm.kv_lens[b], at = len >= end - row ? len - (end - row) : -1;
             if (lane < 2) {
                 void* const base = lane == 0 ? prm.k_ptrs[b] : prm.v_ptrs[b];
                 rows[wave][lane] = at >= 0 ? static_cast<uint16_t*>(base) + (int64_t)at * prm.n_kv_heads * prm.head_dim : nullptr;

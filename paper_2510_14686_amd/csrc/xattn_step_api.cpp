@@ -92,7 +92,9 @@ int xattn_prefill(const void* q, const void* const* k_ptrs, const void* const* v
         return fail(XATTN_EINVAL, "%s: q, k_ptrs, v_ptrs, q_starts, kv_lens and out must not be NULL", who);
     int st = check_prefill(who, batch, total_q, n_q_heads, n_kv_heads, head_dim);
     if (st != XATTN_OK) return st;
-    if (!std::isfinite(scale)) return fail(XATTN_EINVAL, "%s: scale is not finite", who);
+    // The kernel takes a row's maximum ahead of the scale, which must be positive for that.
+    const float scale_log2 = scale == 0.0f ? 1.0f : (float)(std::fabs((double)scale) * 1.4426950408889634074);
+    if (!std::isfinite(scale_log2)) return fail(XATTN_EINVAL, "%s: scale, or scale * log2 e, is not finite", who);
     if (misaligned(q, 16) || misaligned(out, 16)) return fail(XATTN_EINVAL, "%s: q and out must be 16-byte aligned", who);
 
     PrefillParams prm;
@@ -106,8 +108,7 @@ int xattn_prefill(const void* q, const void* const* k_ptrs, const void* const* v
     prm.n_q_heads = n_q_heads;
     prm.n_kv_heads = n_kv_heads;
     prm.group = n_q_heads / n_kv_heads;
-    // The kernel takes a row's maximum ahead of the scale, which must be positive for that.
-    prm.scale_log2 = scale == 0.0f ? 1.0f : (float)(std::fabs((double)scale) * 1.4426950408889634074);
+    prm.scale_log2 = scale_log2;
     prm.q_and = scale == 0.0f ? 0u : 0xffffffffu;
     prm.q_xor = scale < 0.0f ? 0x80008000u : 0u;
     prm.out = static_cast<uint16_t*>(out);
@@ -160,6 +161,9 @@ int xattn_rope_kvcache(const void* q, const void* k_new, const void* v_new, int6
     if (q_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0 || misaligned(q, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) ||
         misaligned(q_out, 16))
         return fail(XATTN_EINVAL, "%s: q, k_new, v_new, q_out and the row strides must be multiples of 16 bytes", who);
+
+    if (q_out == q && q_stride != (int64_t)n_q_heads * head_dim)
+        return fail(XATTN_EINVAL, "%s: q_out may be q only where q's rows are contiguous", who);
 
     RopeParams prm = {};
     prm.q = static_cast<const uint16_t*>(q);

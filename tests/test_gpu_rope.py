@@ -160,6 +160,23 @@ def test_bounds_that_do_not_ascend():
     b.check()
 
 
+def test_lengths_below_the_new_rows():
+    """Down to the least there is: the rows are turned, and not written to the ranges."""
+    b = Batch([(3, 17), (20, 40), (9, 9)], 4, 2, 128, [64], seed=8)
+    for lens in ([-1, 0, 8], [-2 ** 31, -2 ** 31 + 5, -7]):
+        b.kv_lens.copy_(torch.tensor(lens, dtype=torch.int32))
+        b.call()
+        torch.cuda.synchronize()
+        moved = int((b.caches[0] != b.before[0]).any(-1).any(-1).sum())
+        assert moved == (8 if lens[2] == 8 else 0)
+        for c, was in zip(b.caches, b.before):
+            c.copy_(was)
+        b.out.fill_(7)
+    b.kv_lens.copy_(torch.tensor([17, 40, 9], dtype=torch.int32))
+    b.call()
+    b.check()
+
+
 def test_no_rotation_is_write_kvcache():
     """Positions of 0: the same as the plain append, on another batch shape."""
     b = Batch([(2, 9), (2, 30), (2, 2)], 4, 2, 128, [64], seed=6)

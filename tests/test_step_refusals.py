@@ -45,6 +45,15 @@ def test_rope(status, change):
     refused(status, rope, **change)
 
 
+def test_rope_in_place_on_rows_with_gaps():
+    refused(EINVAL, rope, q=A, out=A, qs=1536)
+
+
+def test_prefill_scale_that_overflows():
+    refused(EINVAL, prefill, scale=3e38)
+    refused(EINVAL, prefill, scale=-3e38)
+
+
 def logprobs(logits=A, dtype=0, stride=1000, rows=3, vocab=1000, scale=1.0, tokens=A, k=4, lp=A, top=A, tok=A, lse=A, entropy=A):
     xa.xbeam_logprobs(logits, dtype, stride, rows, vocab, scale, tokens, k, lp, top, tok, lse, entropy)
 
