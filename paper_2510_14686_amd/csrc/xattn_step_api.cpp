@@ -21,6 +21,7 @@ constexpr int kMaxBatch = 4096;
 constexpr int kMaxTotalQ = 1 << 24;
 constexpr int kMaxRowsOfHeads = 1 << 30;      // total_q * n_q_heads
 constexpr int kMaxHeads = 1024;
+constexpr int kMaxRows = 1 << 22;             // of logits: a launch has fewer than 2^32 threads, 512 of them per row
 
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
 
@@ -67,7 +68,7 @@ int check_logprobs(const char* who, int rows, int vocab, int top_k) {
     if (top_k < 0 || top_k > vocab) return fail(XATTN_EINVAL, "%s: top_k %d is not in [0, vocab]", who, top_k);
     if (top_k > kMaxTopK) return fail(XATTN_EUNSUPPORTED, "%s: top_k %d exceeds %d", who, top_k, kMaxTopK);
     if (vocab > 1 << 24) return fail(XATTN_EUNSUPPORTED, "%s: vocab %d exceeds %d", who, vocab, 1 << 24);
-    if (rows > 1 << 24) return fail(XATTN_EUNSUPPORTED, "%s: %d rows exceed %d", who, rows, 1 << 24);
+    if (rows > kMaxRows) return fail(XATTN_EUNSUPPORTED, "%s: %d rows exceed %d", who, rows, kMaxRows);
     return XATTN_OK;
 }
 

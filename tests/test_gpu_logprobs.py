@@ -201,6 +201,30 @@ def test_long_rows_of_a_batch(rows, vocab, dtype, k):
         assert again["top_tok"][2].tolist() == list(range(k)) and 11 not in again["top_tok"][1].tolist()
 
 
+def test_the_most_rows():
+    logits = normal(2 ** 22, 3, torch.float32, seed=11)
+    r = run(logits, 2)
+    torch.cuda.synchronize()
+    x = logits.double()
+    lse = torch.logsumexp(x, 1)
+    lp = x - lse[:, None]
+    tol = (400 * U) * (4 + x.abs().amax(1))
+    assert bool(((r["lse"].double() - lse).abs() <= tol).all())
+    assert bool(((r["token_lp"].double() - lp.gather(1, r["tokens"].long()[:, None])[:, 0]).abs() <= tol).all())
+    best = x.sort(dim=1, descending=True, stable=True).indices[:, :2]
+    assert torch.equal(r["top_tok"].long(), best)
+    assert bool(((r["top_lp"].double() - lp.gather(1, best)).abs() <= tol[:, None]).all())
+
+
+@pytest.mark.parametrize("dtype", list(KINDS), ids=str)
+def test_the_longest_row(dtype):
+    logits = normal(1, 2 ** 24, dtype, seed=12)
+    logits[0, -1] = 14.0
+    r = run(logits, 30)
+    check(logits, 30, r)
+    assert r["top_tok"][0, 0].item() == 2 ** 24 - 1
+
+
 def test_zeros_of_both_signs_are_equal():
     logits = torch.full((1, 5000), -1.0, device="cuda")
     logits[0, 100:200:2], logits[0, 101:200:2] = -0.0, 0.0

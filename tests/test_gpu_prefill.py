@@ -118,6 +118,13 @@ def test_wide_groups():
         check(s)
 
 
+@pytest.mark.parametrize("hq,hkv", [(1024, 1), (1024, 1024), (1023, 3)])
+def test_the_most_heads(hq, hkv):
+    s = make([(2, 70), (1, 200), (3, 3)], hq, hkv, seed=hkv)
+    call(s)
+    check(s)
+
+
 @pytest.mark.parametrize("scale", [-0.09, 0.0, 1.0, 1e-4])
 def test_scales(scale):
     s = make([(70, 150), (1, 1000), (33, 33)], 8, 2, seed=7)

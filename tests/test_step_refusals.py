@@ -69,6 +69,12 @@ def test_logprobs(status, change):
     refused(status, logprobs, **change)
 
 
+def test_logprobs_of_more_rows_than_a_launch_has_threads_for():
+    refused(EUNSUPPORTED, logprobs, rows=2 ** 22 + 1)
+    with pytest.raises(xa.XattnError):
+        xa.xbeam_logprobs_workspace_bytes(2 ** 22 + 1, 1000, 0)
+
+
 def test_arguments_that_are_no_numbers_or_tensors():
     for fn, bad in ((prefill, dict(q="x")), (prefill, dict(scale="x")), (rope, dict(pos=1.5)), (rope, dict(sections=(6.5,))), (logprobs, dict(scale=None))):
         with pytest.raises(TypeError):
