@@ -62,7 +62,8 @@ int xbeam_select(const float* beam_lp, const float* cand_lp, const int32_t* cand
  * Logits of -inf, or of a type's lowest value, are forbidden tokens: probability 0 beside others, last among the alternatives.  In a row
  * of nothing but -inf, lse is -inf, entropy and log-probabilities are NaN, the alternatives are the first indices.  With +inf in a
  * row, or NaN, lse, entropy and log-probabilities are NaN; a NaN is no alternative: where a row has fewer than top_k others,
- * the rest of top_tok is -1 (top_lp NaN).  Sums are kept in fp32.
+ * the rest of top_tok is -1 (top_lp NaN).  Sums are kept in fp32, of differences of logits: how far a row lies from 0 takes no digits of
+ * its log-probabilities and entropy, and no log-probability is above 0.
  * rows 1..2^22, vocab 1..2^24.  Asynchronous on `stream`, which it may be captured on.  Where rows are few they are cut into parts, whose
  * results meet in the stream's workspace (xattn_set_workspace; xbeam_logprobs_workspace_bytes: what one call needs of it),
  * with the rules that xattn_decode states.

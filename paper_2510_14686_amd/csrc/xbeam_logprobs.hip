@@ -29,7 +29,9 @@ namespace {
 
 constexpr int kVals = kLoads * kStep / 64;       // a lane's values in a round
 constexpr int kAtOnce = -1;
-constexpr float kFar = 1e30f;                    // logits beyond are summed up in a second pass, whose differences do not overflow
+// Rows whose maximum, in log2 units, is this far from 0 are summed up in a second pass, of differences of logits: a reference is off by half of its
+// last digit, which is up to 2^-1 here.
+constexpr float kFar = 16777216.0f;
 
 // Bits that order as the values do; NaN below everything (0), -0 as 0.
 __device__ __forceinline__ uint32_t order_key(float x) {
@@ -65,17 +67,30 @@ template <typename T> struct Chunk {
     }
 };
 
-// m, s and t of some values; m is finite.
+// s and t of some values, and what they are relative to.  While a row is read that is the reference r = m * c as rounded: y = x * c - r is one
+// operation per value, whose terms belong to r itself, so that the sums of lanes and waves meet at the differences of their r, whatever
+// m * c lost in rounding.  (Taken for m * c, r is off by 2^-24 of it: logits 10^5 from 0 had log-probabilities 5e-3 off.)  A whole row's sums are
+// relative to its maximum m.
 struct Sums {
     float m, s, t;
 };
-__device__ __forceinline__ void move_to(Sums& a, float m, float c) {
-    const float d = fmaxf((a.m - m) * c, -1e30f), f = fast_exp2(d);
+__device__ __forceinline__ void move_by(Sums& a, float m, float d) {      // d: from there to m in log2 units
+    d = fmaxf(d, -1e30f);
+    const float f = fast_exp2(d);
     a.t = f * (a.t + d * a.s);
     a.s *= f;
     a.m = m;
 }
-__device__ __forceinline__ void add(Sums& a, float y) {      // y = (x - m) * c
+__device__ __forceinline__ void move_reference(Sums& a, float r) { move_by(a, r, a.m - r); }
+__device__ __forceinline__ void move_to(Sums& a, float m, float c) { move_by(a, m, (a.m - m) * c); }
+// From the reference of m to m itself.  Divided by the weight that m has, the sum is 1 at least, and exactly 1 where nothing is beside m.
+__device__ __forceinline__ void settle(Sums& a, float m, float c) {
+    const float d = __builtin_fmaf(m, c, -a.m), w = fast_exp2(d);
+    a.t = (a.t - d * a.s) / w;
+    a.s /= w;
+    a.m = m;
+}
+__device__ __forceinline__ void add(Sums& a, float y) {      // y = x * c - r
     const float e = fast_exp2(y);
     a.s += e;
     a.t = __builtin_fmaf(e, fmaxf(y, -1000.0f), a.t);        // e is 0 from -150 on, and -inf times that no number
@@ -475,11 +490,10 @@ __global__ __launch_bounds__(64 * kWaves, kCap == kAtOnce ? 8 : 4) void logprobs
         }
         if (__ballot(all > top) != 0) {
             top = fmaxf(top, all);
-            move_to(a, fmaxf(top, -kFar), c);
+            move_reference(a, fmaxf(top * c, -kFar));
         }
-        const float mc = a.m * c;
 #pragma unroll
-        for (int i = 0; i < kVals; ++i) add(a, __builtin_fmaf(x[i], c, -mc));
+        for (int i = 0; i < kVals; ++i) add(a, __builtin_fmaf(x[i], c, -a.m));
         if constexpr (kList) {
             if ((round & (round - 1)) == 0 && (round & 0x2aaaaaaa) == 0) {      // rounds 0, 1, 4, 16, ...
                 raise();
@@ -522,8 +536,7 @@ __global__ __launch_bounds__(64 * kWaves, kCap == kAtOnce ? 8 : 4) void logprobs
     }
     const float wave_top = wave_max(top);
     {
-        const float m = fmaxf(wave_top, -kFar);
-        move_to(a, m, c);
+        move_reference(a, fmaxf(wave_top * c, -kFar));
         a.s = wave_sum(a.s);
         a.t = wave_sum(a.t);
     }
@@ -535,15 +548,16 @@ __global__ __launch_bounds__(64 * kWaves, kCap == kAtOnce ? 8 : 4) void logprobs
     float row_top = tops[0];
 #pragma unroll
     for (int i = 1; i < kWaves; ++i) row_top = fmaxf(row_top, tops[i]);
-    Sums r = {fmaxf(row_top, -kFar), 0.0f, 0.0f};
+    Sums r = {fmaxf(row_top * c, -kFar), 0.0f, 0.0f};
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
         Sums x = partial[i];
-        move_to(x, r.m, c);
+        move_reference(x, r.m);
         r.s += x.s;
         r.t += x.t;
     }
-    if (__builtin_fabsf(row_top) >= kFar && __builtin_fabsf(row_top) < __builtin_inff()) {
+    if (__builtin_fabsf(row_top * c) < kFar) settle(r, row_top, c);
+    else if (__builtin_fabsf(row_top) < __builtin_inff()) {
         __syncthreads();
         a = Sums{row_top, 0.0f, 0.0f};
         for (int i = begin + tid; i < end; i += 64 * kWaves) add(a, (to_float(logits[i]) - row_top) * c);
