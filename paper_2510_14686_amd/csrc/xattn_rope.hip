@@ -20,8 +20,6 @@
 namespace xattn {
 namespace {
 
-constexpr int kRopeThreads = 256;
-
 // The sequence whose rows [q_starts[b], q_starts[b + 1]) hold `row`, and where its new rows begin and end; -1 without one.
 // Wave-uniform: each lane looks at the bounds of batch / 64 sequences, then of one.
 __device__ __forceinline__ int find_sequence(const int32_t* __restrict__ q_starts, int batch, int row, int lane, int& start, int& end) {
@@ -157,13 +155,11 @@ hipError_t launch_rope(const RopeParams& prm, hipStream_t stream) {
         return prm.head_dim == 128 ? launch(rope_kernel<kTokens, 8>, grid, kRopeThreads, stream, prm)
                                    : launch(rope_kernel<kTokens, 0>, grid, kRopeThreads, stream, prm);
     };
-    // A workgroup of few short rows has threads without work, one of more rows than its threads need moves them in more turns of its loop.
-    // Of 1 / 2 / 4 rows each, in us: 256 rows of 40 / 8 heads 5.8 / 6.5 / 8.4, 2000 rows 13.1 / 12.2 / 13.2, 16384 rows 86.4 / 89.0 / 95.1; 16384
-    // of 64 / 8 heads 120 / 127 / 135, of 16 / 8 47.2 / 41.7 / 43.5; 65536 of 8 / 1 139 / 90 / 69.
-    const int items = (prm.n_q_heads + 2 * prm.n_kv_heads) * (prm.head_dim / 16);      // of a row
-    return prm.total_q < 1024 || items > 2 * kRopeThreads ? with(std::integral_constant<int, 1>())
-           : items > kRopeThreads / 2                     ? with(std::integral_constant<int, 2>())
-                                                          : with(std::integral_constant<int, 4>());
+    switch (rope_rows_per_workgroup(prm.total_q, prm.n_q_heads, prm.n_kv_heads, prm.head_dim)) {
+        case 1: return with(std::integral_constant<int, 1>());
+        case 2: return with(std::integral_constant<int, 2>());
+        default: return with(std::integral_constant<int, 4>());
+    }
 }
 
 }  // namespace xattn
