@@ -154,8 +154,8 @@ int xattn_mla_decode(const void* q, const void* const* c_ptrs, const int32_t* kv
  * 1024, a multiple of n_kv_heads.  Otherwise XATTN_EUNSUPPORTED.  scale and scale * log2 e finite.
  * out      DEVICE  bf16 [total_q, n_q_heads, head_dim], 16-byte aligned, not overlapping the inputs;  lse DEVICE fp32 [total_q, n_q_heads] or NULL
  * Same stream, capture and ownership rules as xattn_decode, same workspace (of at least xattn_prefill_workspace_bytes).
- * Numerics: scores, maxima and sums in fp32; a softmax weight enters the value product as one bf16 (off by 2^-8 of it at most,
- * xattn_decode keeps 24 bits), the result is rounded to bf16 once.  q and the keys and values of a sequence must be finite: an
+ * Numerics: scores, maxima and sums in fp32; a softmax weight enters the value product as one bf16 (off by 2^-8 of it at most)
+ * or, with XATTN_CFG_PV_MODE = 1, with all its 24 bits as in xattn_decode; the result is rounded to bf16 once.  q and the keys and values of a sequence must be finite: an
  * infinity or NaN leaves the sequence's rows unspecified, and no others.
  */
 int xattn_prefill(const void* q, const void* const* k_ptrs, const void* const* v_ptrs, const int32_t* q_starts,
@@ -222,6 +222,8 @@ int xattn_set_workspace(void* dev_ptr, size_t bytes);
  *                               cuts the number of pieces) and wherever a key carries 1/4 or more of its
  *                               row's running sum, one bf16 elsewhere; 1 = hi + lo parts everywhere;
  *                               2 = one bf16 per weight everywhere, less exact on peaked rows)
+ *                               (xattn_prefill: 0 and 2 = one bf16 per weight; 1 = three bf16 parts, all 24
+ *                               significant bits, for 1.7 times the time of a prompt)
  *   XATTN_CFG_MLA_LAYOUT        xattn_mla_decode workgroup shape: 0 = automatic (up to 32 query rows per
  *                               sequence four waves share a 16-row tile; then 32-row tiles, 4 waves,
  *                               one or, in short pieces, two per tile), 1 = one 16-row tile per wave, up to 4 waves, for any number of

@@ -258,6 +258,8 @@ int with_workspace(const char* who, size_t bytes, void* stream, WorkspaceLaunchF
     return st != XATTN_OK ? st : launch(context, ws);
 }
 
+int configured_pv_mode() { return g_cfg_pv_mode; }
+
 // xattn_decode and its variants: argument checks, workspace, launch.  `fixed_workspace`, when given,
 // supplies the workspace instead of the per-stream one (and the call is never timed: events allocate).
 int decode_call(const char* who, FixedWorkspaceFn fixed_workspace, const void* q, const void* const* k_ptrs,

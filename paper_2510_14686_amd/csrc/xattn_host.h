@@ -20,6 +20,8 @@ int decode_call(const char* who, FixedWorkspaceFn fixed_workspace, const void* q
 // one call together.
 typedef int (*WorkspaceLaunchFn)(void* context, char* workspace);
 int with_workspace(const char* who, size_t bytes, void* stream, WorkspaceLaunchFn launch, void* context);
+// XATTN_CFG_PV_MODE, for a launch under that lock.
+int configured_pv_mode();
 
 }  // namespace xattn
 #endif

@@ -24,6 +24,7 @@ struct PrefillParams {
     float* part_ml;                  // fp32 [kPrefillSlots, slot_rows, 2]: reference maximum (log2 domain), sum
     float* part_o;                   // fp32 [kPrefillSlots, slot_rows, 128]
     int slot_rows;
+    int exact;                       // weights enter the product with V with all their bits
 };
 constexpr size_t kPrefillTableBytes = 32 + 32 * (size_t)kPrefillShares;
 hipError_t launch_prefill(const PrefillParams& prm, hipStream_t stream);

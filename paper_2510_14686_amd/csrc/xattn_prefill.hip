@@ -16,8 +16,10 @@
 // its rows interleaved, the prompt of 16001 takes 2200 us where this takes 1845, and one of 2048 77 us where this takes 49.
 //   32 keys at a time make the weights beside the next scores: with 64 the two sets of scores do not fit, and in turn, without
 // the overlap, 2246 us where this took 2004 then.
-//   Weights enter the second product as one bf16 each, off by 2^-8 of it at most, as the values of V themselves may be: two or three
-// parts of them, as a decode step takes, would double or treble the products with V that bound this.
+//   Weights enter the second product as one bf16 each, off by 2^-8 of it at most, as the values of V themselves may be.  On request (kExact)
+// as three bf16 parts, all 24 bits of them: the prompt of 16001 takes 1.72 times as long, 64 sequences of 4096 and one new token each 172 us
+// instead of 170, a prompt of 1000 among decoding sequences 138 instead of 122, four short sequences 12.9 instead of 10.8 (the products
+// are a part of each step's latency there).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -188,6 +190,7 @@ __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(0)"
 // 16 keys of step s in O^T += V^T P^T.
 __device__ __forceinline__ int tile_row(int x) { return (x & ~12) | ((x & 4) << 1) | ((x & 8) >> 1); }
 
+template <bool kExact>
 __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams prm) {
     __shared__ __attribute__((aligned(1024))) char lds[2 * 2 * kBlockBytes];      // K, K, V, V
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6);
@@ -339,6 +342,23 @@ __global__ __launch_bounds__(64 * kWaves, 2) void prefill_kernel(PrefillParams p
                                                                      cvt_bf16(p[8 * st + 4], p[8 * st + 5]), cvt_bf16(p[8 * st + 6], p[8 * st + 7])});
 #pragma unroll
             for (int c = 0; c < 4; ++c) o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[st][c], pb, o[c], 0, 0, 0);
+            if constexpr (kExact) {
+                // What bf16 leaves of the weights, then what it leaves of that.
+                u32x4_t part = __builtin_bit_cast(u32x4_t, pb);
+#pragma unroll
+                for (int again = 0; again < 2; ++again) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float &a = p[8 * st + 2 * i], &b = p[8 * st + 2 * i + 1];
+                        a -= bf16_lo(part[i]);
+                        b -= bf16_hi(part[i]);
+                        part[i] = cvt_bf16(a, b);
+                    }
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        o[c] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(va[st][c], __builtin_bit_cast(bf16x8_t, part), o[c], 0, 0, 0);
+                }
+            }
         }
     };
 
@@ -485,7 +505,7 @@ __global__ __launch_bounds__(64 * kMergeWaves) void prefill_merge_kernel(Prefill
 
 hipError_t launch_prefill(const PrefillParams& prm, hipStream_t stream) {
     const long grid = prefill_grid(prm.total_q, prm.batch, prm.group, prm.n_kv_heads);
-    hipError_t e = launch(prefill_kernel, dim3((unsigned)grid), 64 * kWaves, stream, prm);
+    hipError_t e = launch(prm.exact ? prefill_kernel<true> : prefill_kernel<false>, dim3((unsigned)grid), 64 * kWaves, stream, prm);
     if (e != hipSuccess) return e;
     return launch(prefill_merge_kernel, dim3(kMergeGroups), 64 * kMergeWaves, stream, prm);
 }

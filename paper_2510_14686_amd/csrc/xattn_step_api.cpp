@@ -126,6 +126,7 @@ int xattn_prefill(const void* q, const void* const* k_ptrs, const void* const* v
         c.prm->table = reinterpret_cast<int32_t*>(ws);
         c.prm->part_ml = reinterpret_cast<float*>(ws + c.ml_off);
         c.prm->part_o = reinterpret_cast<float*>(ws + c.o_off);
+        c.prm->exact = configured_pv_mode() == 1;
         const hipError_t e = launch_prefill(*c.prm, c.stream);
         return e == hipSuccess ? (int)XATTN_OK : fail_hip(e, "kernel launch");
     }, &call);
