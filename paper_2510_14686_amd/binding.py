@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from operator import index
 from typing import Optional, Tuple
 
 import numpy as np
@@ -329,7 +330,7 @@ _sections_arrays = {}      # the C arrays of the sections that calls have named 
 
 
 def _sections_array(sections):
-    key = tuple(sections)
+    key = tuple(map(index, sections))
     array = _sections_arrays.get(key)
     if array is None:
         array = (ctypes.c_int * len(key))(*key)
