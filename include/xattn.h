@@ -70,15 +70,16 @@ const char* xattn_last_error(void);
  * scale    multiplies the scores before the softmax (the caller's fp32 value, e.g. 1/sqrt(128))
  * out      DEVICE  bf16 [batch, q_len, n_q_heads, head_dim]
  * lse      DEVICE  fp32 [batch, q_len, n_q_heads], natural log; may be NULL
- * stream   hipStream_t (NULL = the default stream).  The call only enqueues work: it never
- *          synchronises and never reads device memory on the host.
+ * stream   hipStream_t (NULL = the default stream) of the current device, whose workspace the call takes.  The call only
+ *          enqueues work: it never synchronises and never reads device memory on the host.
  *
  * Graph capture (section 4.2, "Integrating Custom Operators"): the call may be recorded into a HIP
  * graph and replayed with other lengths, pointers and data in the same device buffers, since nothing
  * on the host depends on their values.  The stream's workspace must be large enough beforehand (one
  * eager call of the shape ON THAT STREAM, or xattn_set_workspace); a call that would have to grow it
  * during capture returns XATTN_ENOMEM and records nothing.  A recorded graph stays valid when later
- * calls grow the workspace: outgrown buffers are kept until the process ends, never freed.
+ * calls grow the workspace: outgrown buffers are kept until the process ends, never freed.  It keeps using the workspace of
+ * the stream that it was recorded on: replays on other streams must not overlap calls on that one, or each other.
  *
  * Ownership: the caller owns every buffer and keeps it alive and unmodified until the enqueued work
  * has finished.  The library keeps one workspace per stream (see below), so calls on different
@@ -168,7 +169,9 @@ int xattn_prefill(const void* q, const void* const* k_ptrs, const void* const* v
  * xattn_workspace_bytes:     upper bound on the bytes one xattn_decode call of this shape uses
  *                            (0 and a message for an unsupported shape).
  * xattn_mla_workspace_bytes: the same for one xattn_mla_decode call.
- * xattn_prefill_workspace_bytes: the same for one xattn_prefill call, which takes no less than that.
+ * xattn_prefill_workspace_bytes: the same for one xattn_prefill call, which takes no less than that: 65 MiB from
+ *                            total_q * n_q_heads / n_kv_heads = 128 on, whether or not sequences are split, so the
+ *                            first such call on a stream outgrows what xattn_decode had there.
  * xattn_set_workspace:       hand the library a DEVICE buffer (256-byte aligned) for the current
  *                            device, used by calls on every stream; the caller keeps ownership and
  *                            keeps it alive while calls are in flight or graphs that recorded them

@@ -8,7 +8,7 @@
 // group, and a tile of a short sequence holds all its rows.
 //
 // Many new tokens are bound by the matrix pipes at the clock that the card's power leaves them: one prompt of 16001, 32 / 8 heads,
-// 1.85 to 1.95 ms, 1080 to 1140 TFLOP/s, against the 1360 of a bf16 matrix product of 16384 in a library; the pipes are busy 60 % of the
+// 1.85 to 1.95 ms, 1080 to 1140 TFLOP/s, against the 1360 of a bf16 matrix product of 16384 in a library; the pipes are busy 64 % of the
 // time at 1.6 GHz.  Few are bound by reading the keys: 64 sequences of 4096 and one new token each, 171 us, 6.3 TB/s.  A handful of
 // short sequences takes 9 us of finding the work and a few blocks' latencies, and 2 us of merge.
 //   A wave has 32 rows, so that its scores, weights and sums need 200 registers and two waves share a SIMD, one in its softmax while

@@ -3,8 +3,8 @@
 //   x = scale * logit;  s = sum exp(x - m), t = sum (x - m) exp(x - m);  lse = m + ln s;  lp = x - lse;  H = ln s - t / s
 //
 // A row is read once.  Every lane keeps m (its own maximum), s and t of its values, moved on when m moves, and the lanes' are put together at
-// the end.  Long rows are bound by the instructions beside the reading, eleven per value: 4096 rows of 131072 bf16 logits, 5 alternatives, 187
-// us, 5.7 TB/s, the vector units busy 92 % of the time.  Short rows with many alternatives are bound by picking and ordering them: 1024 rows of
+// the end.  Long rows are bound by the instructions beside the reading, eleven per value: 4096 rows of 131072 bf16 logits, 5 alternatives, 191
+// us, 5.6 TB/s, the vector units busy 99 % of the time.  Short rows with many alternatives are bound by picking and ordering them: 1024 rows of
 // 8192 fp32 logits, 512 alternatives, 25 us, of which the sums take 9, marking what may be one of the best 6, picking 6 and ordering 4.
 //
 // Alternatives: a lane's maximum is there anyway, and if in each of some waves ceil(k / 8) lanes have a maximum of tau or more, and
