@@ -161,6 +161,12 @@ struct WavePlan {
     int mine;                // stream positions of this lane's sequences
     int excl;                // stream positions before this lane's first sequence
 };
+// What a sequence of `raw` tokens (any sign) takes of the stream: a position per token.
+struct TokenUnit {
+    static __device__ __forceinline__ int positions(int raw) { return clamp_len(raw); }
+    static __device__ __forceinline__ int stream(int raw, int seg_cost) { return stream_len(raw, seg_cost); }
+};
+
 // Lengths and base addresses of up to 64 consecutive sequences, one per lane: those around the
 // position a wave starts at, fetched in the same round trips as the plan, so that a segment's first
 // K/V loads do not wait for another two dependent loads (its length, then its pointers).
@@ -174,6 +180,7 @@ __device__ __forceinline__ u32x2_t load_ptr_entry(const void* const* ptrs, int b
     const __amdgpu_buffer_rsrc_t r = make_rsrc(ptrs, (uint32_t)batch * 8u);
     return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_raw_buffer_load_b64(r, idx * 8, 0, 0));
 }
+template <typename Unit = TokenUnit>
 __device__ __forceinline__ void window_load(SeqWindow& win, const int32_t* __restrict__ kv_lens, const void* const* k_ptrs,
                                             const void* const* v_ptrs, int batch, int base, int count, int lane,
                                             int seg_cost, int& positions) {
@@ -185,7 +192,7 @@ __device__ __forceinline__ void window_load(SeqWindow& win, const int32_t* __res
     win.base = base;
     win.count = count;
     win.len = clamp_len(raw);
-    positions = stream_len(raw, seg_cost);
+    positions = Unit::stream(raw, seg_cost);
 }
 // Length and pointers of sequence b: from the window when it holds b, else from memory.  Wave-uniform.
 __device__ __forceinline__ int window_len(const SeqWindow& win, const int32_t* __restrict__ kv_lens, int b) {
@@ -209,6 +216,7 @@ __device__ __forceinline__ const void* window_ptr(const SeqWindow& win, const u3
 }
 
 // Stream positions of up to 16 sequences, `count` of them (a multiple of four) from `first` on.
+template <typename Unit = TokenUnit>
 __device__ __forceinline__ int chunk_positions(__amdgpu_buffer_rsrc_t rl, int first, int count, int seg_cost) {
     u32x4_t v[4];
 #pragma unroll
@@ -216,13 +224,14 @@ __device__ __forceinline__ int chunk_positions(__amdgpu_buffer_rsrc_t rl, int fi
     int sum = 0;
 #pragma unroll
     for (int k = 0; k < 4; ++k)
-        sum += stream_len((int)v[k].x, seg_cost) + stream_len((int)v[k].y, seg_cost) +
-               stream_len((int)v[k].z, seg_cost) + stream_len((int)v[k].w, seg_cost);
+        sum += Unit::stream((int)v[k].x, seg_cost) + Unit::stream((int)v[k].y, seg_cost) +
+               Unit::stream((int)v[k].z, seg_cost) + Unit::stream((int)v[k].w, seg_cost);
     return sum;
 }
 
 // win (optional): with at most 64 sequences (one per lane) the window is filled here, in the plan's own
 // round trip.
+template <typename Unit = TokenUnit>
 __device__ __forceinline__ WavePlan wave_plan(const int32_t* __restrict__ kv_lens, const void* const* k_ptrs,
                                               const void* const* v_ptrs, int batch, int n_pieces, int min_piece,
                                               int seg_cost, int xcd_skew, FewPieces few, int lane, SeqWindow* win, int parts = 1) {
@@ -239,8 +248,8 @@ __device__ __forceinline__ WavePlan wave_plan(const int32_t* __restrict__ kv_len
         win->count = 0;
     }
     if (lg == 0) {
-        if (win) window_load(*win, kv_lens, k_ptrs, v_ptrs, batch, 0, batch, lane, seg_cost, mine);
-        else mine = stream_len(__builtin_amdgcn_raw_buffer_load_b32(rl, first * 4, 0, 0), seg_cost);
+        if (win) window_load<Unit>(*win, kv_lens, k_ptrs, v_ptrs, batch, 0, batch, lane, seg_cost, mine);
+        else mine = Unit::stream(__builtin_amdgcn_raw_buffer_load_b32(rl, first * 4, 0, 0), seg_cost);
     } else {
         // Four lengths, at chunk 2 the last two are the next lane's; of longer chunks sixteen more at a time, the first of
         // them in the same round trip.  (A form for every chunk size is code that all calls jump across: of 16 to 100 tokens and 2
@@ -248,9 +257,9 @@ __device__ __forceinline__ WavePlan wave_plan(const int32_t* __restrict__ kv_len
         // for the longest chunks 28.7, 35.3, 60.8.)
         const u32x4_t v = __builtin_amdgcn_raw_buffer_load_b128(rl, first * 4, 0, 0);
         mine = 0;
-        for (int k = 4; k < wp.chunk; k += 16) mine += chunk_positions(rl, first + k, wp.chunk - k, seg_cost);
-        mine += stream_len((int)v.x, seg_cost) + stream_len((int)v.y, seg_cost);
-        if (lg > 1) mine += stream_len((int)v.z, seg_cost) + stream_len((int)v.w, seg_cost);
+        for (int k = 4; k < wp.chunk; k += 16) mine += chunk_positions<Unit>(rl, first + k, wp.chunk - k, seg_cost);
+        mine += Unit::stream((int)v.x, seg_cost) + Unit::stream((int)v.y, seg_cost);
+        if (lg > 1) mine += Unit::stream((int)v.z, seg_cost) + Unit::stream((int)v.w, seg_cost);
     }
     const int incl = wave_incl_scan_i(mine);
     wp.mine = mine;
@@ -262,6 +271,7 @@ __device__ __forceinline__ WavePlan wave_plan(const int32_t* __restrict__ kv_len
 // The sequence b that holds stream position s (0 <= s < N) and the offset j of s within that
 // sequence's L + seg_cost positions.  Both wave-uniform.  With more than 64 sequences the window is
 // filled here with the located chunk.
+template <typename Unit = TokenUnit>
 __device__ __forceinline__ void wave_locate(const WavePlan& wp, const int32_t* __restrict__ kv_lens, const void* const* k_ptrs,
                                             const void* const* v_ptrs, int batch, int s, int lane, SeqWindow* win, int& b,
                                             int& j) {
@@ -276,10 +286,10 @@ __device__ __forceinline__ void wave_locate(const WavePlan& wp, const int32_t* _
     const int base = ln << wp.chunk_log2;
     int v;
     if (win) {
-        window_load(*win, kv_lens, k_ptrs, v_ptrs, batch, base, wp.chunk, lane, wp.pl.seg_cost, v);
+        window_load<Unit>(*win, kv_lens, k_ptrs, v_ptrs, batch, base, wp.chunk, lane, wp.pl.seg_cost, v);
     } else {
         const __amdgpu_buffer_rsrc_t rl = make_rsrc(kv_lens, (uint32_t)batch * 4u);
-        v = lane < wp.chunk ? stream_len(__builtin_amdgcn_raw_buffer_load_b32(rl, (base + lane) * 4, 0, 0), wp.pl.seg_cost) : 0;
+        v = lane < wp.chunk ? Unit::stream(__builtin_amdgcn_raw_buffer_load_b32(rl, (base + lane) * 4, 0, 0), wp.pl.seg_cost) : 0;
     }
     const int incl = wave_incl_scan_i(v);
     const unsigned long long hit2 = __ballot(off >= incl - v && off < incl);
@@ -291,6 +301,7 @@ __device__ __forceinline__ void wave_locate(const WavePlan& wp, const int32_t* _
 // For the merge kernel: (first partial slot, number of segments) of sequences 64 g .. 64 g + 63, one
 // per lane.  A group of 64 sequences holds 64 / chunk whole chunks; a sequence's first position is its
 // chunk's first position plus the positions of the chunk's earlier sequences.
+template <typename Unit = TokenUnit>
 __device__ __forceinline__ void wave_write_meta(const WavePlan& wp, const int32_t* __restrict__ kv_lens, int batch, int seq_rows, int g,
                                                 int lane, int32_t* __restrict__ meta) {
     const int seq = 64 * g + lane;
@@ -305,8 +316,8 @@ __device__ __forceinline__ void wave_write_meta(const WavePlan& wp, const int32_
     const int until = __builtin_amdgcn_update_dpp(0, from, 0x101, 0xf, 0xf, false);      // lane x + 1's
     const bool spread = n >= 8 && __ballot(x < 8 && large_part(pl, until - from, rows)) != 0;
     __builtin_amdgcn_sched_barrier(0);
-    const int len = clamp_len(raw);
-    const int v = stream_len(len, wp.pl.seg_cost);
+    const int len = Unit::positions(raw);
+    const int v = len > 0 ? len + wp.pl.seg_cost : 0;
     const int before = wave_incl_scan_i(v) - v;                       // within the group
     const int chunk_first = __shfl(wp.excl, (seq >> wp.chunk_log2) & 63, 64);
     const int start = chunk_first + before - __shfl(before, lane & ~(wp.chunk - 1), 64);

@@ -69,6 +69,8 @@ int rows_per_wave(int rows_total, int path);
 // Enqueues the split-KV decode kernel and the merge kernel on `stream`.  If `events` is not null it
 // holds three events, recorded before the decode kernel, between the kernels and after the merge.
 hipError_t launch_decode(const DecodeParams& prm, hipStream_t stream, hipEvent_t* events);
+// The merge kernel alone, behind a decode kernel that left its partial results in prm.part_o, part_ml and meta.
+hipError_t launch_decode_merge(const DecodeParams& prm, hipStream_t stream);
 
 // Waves per output row of the merge kernels: as many as keep the launch within what the chip holds at once
 // (256 compute units of 32 waves).  Few rows mean few sequences, whose keys may be split into hundreds of
