@@ -387,6 +387,44 @@ int xattn_rope_kvcache(const void* q, const void* k_new, const void* v_new, int6
                        void* const* k_ptrs, void* const* v_ptrs, const int32_t* q_starts, const int32_t* kv_lens, int batch,
                        int total_q, int n_q_heads, int n_kv_heads, int head_dim, void* q_out, void* stream);
 
+/*
+ * KV cache of 4 bits a value.  A head's row of 128 values is four blocks of 32, each with a scale 2^e (a byte, e + 127), and a value is one of 0,
+ * 0.5, 1, 1.5, 2, 3, 4, 6 times that, with a sign (e2m1 elements and e8m0 scales of the OCP Microscaling Formats): 68 bytes a row instead of
+ * 256.  e is the least from -125 to 126 with every value within 7 * 2^e; a value goes to the nearest code, of two as near to the even one.  A
+ * block with a NaN or an infinity is stored as NaN (scale byte 255).
+ * Ranges hold tiles of XATTN_MX_TILE_TOKENS tokens: tile i of KV head h is at (i * n_kv_heads + h) * XATTN_MX_TILE_BYTES and has token t = 16 s + u of
+ * it (0 <= u < 16), the lower half of a byte first:
+ *     K  codes of values 32 c .. + 31 at 1024 s + 256 c + 16 u                 scale of block c at 4096 + 4 (16 c + u) + s
+ *     V  codes of values 8 m .. + 7 at 1024 s + 256 (u / 4) + 16 m + 4 (u % 4)   scale of block c at 4096 + 16 (4 (u / 4) + c) + 4 s + u % 4
+ * A range is 16-byte aligned, and backed in whole tiles: xattn_mx_range_bytes(tokens, n_kv_heads, 128) bytes for so many tokens.  What stands
+ * in a tile behind the last token may be anything.  A sequence's K may exceed 4 GiB.
+ *
+ * xattn_mx_range_bytes   0 tokens: 0.  0 and a message for sizes that are not supported (1..1024 heads, head_dim 128).
+ * xattn_rope_kvcache_mx  xattn_rope_kvcache, arguments and checks alike, but into such ranges: K is rotated in double and stored as codes from
+ *                        there (no rounding in between), V as it is.  head_dim 128.  Rows are written whole, and nothing else is.
+ * xattn_read_kvcache_mx  the packed rows of a batch as bf16, exactly what the codes stand for: row q_starts[b] + t of k_out and v_out
+ *                        [total_q, n_kv_heads, 128] (16-byte aligned) is row kv_lens[b] - q_len + t of sequence b, with q_len = q_starts[b + 1] -
+ *                        q_starts[b]; all rows where that is kv_lens[b].  Rows before the first are zeros; rows from q_starts[batch] on are left
+ *                        as they were.  (A prompt's chunk behind a cached part: read all rows, attend them with xattn_prefill.)
+ *                        Bounds and limits as for xattn_rope_kvcache.
+ * xattn_decode_mx        xattn_decode over such ranges: same arguments, shapes, masks, outputs, stream, capture and ownership rules, and the
+ *                        same workspace, of at least xattn_decode_mx_workspace_bytes.  scale * log2 e finite.  K and V enter the products
+ *                        exactly; scores, maxima and sums are fp32; a softmax weight enters the value product as two bf16 (16 significant bits).
+ *                        A NaN or an infinity in a sequence's rows or queries leaves its results unspecified, and no others.  XATTN_CFG_* do not apply.
+ */
+#define XATTN_MX_TILE_TOKENS 64
+#define XATTN_MX_TILE_BYTES 4352
+size_t xattn_mx_range_bytes(int64_t tokens, int n_kv_heads, int head_dim);
+int xattn_rope_kvcache_mx(const void* q, const void* k_new, const void* v_new, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                          const int32_t* pos, const float* inv_freq, const int32_t* sections, int n_axes, int flags,
+                          void* const* k_ptrs, void* const* v_ptrs, const int32_t* q_starts, const int32_t* kv_lens, int batch,
+                          int total_q, int n_q_heads, int n_kv_heads, int head_dim, void* q_out, void* stream);
+int xattn_read_kvcache_mx(const void* const* k_ptrs, const void* const* v_ptrs, const int32_t* q_starts, const int32_t* kv_lens, int batch,
+                          int total_q, int n_kv_heads, int head_dim, void* k_out, void* v_out, void* stream);
+int xattn_decode_mx(const void* q, const void* const* k_ptrs, const void* const* v_ptrs, const int32_t* kv_lens, int batch, int q_len,
+                    int n_q_heads, int n_kv_heads, int head_dim, float scale, void* out, float* lse, void* stream);
+size_t xattn_decode_mx_workspace_bytes(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim);
+
 /* Synchronous copies between HOST memory and any DEVICE address (mapped ranges included). */
 int xtensor_upload(void* dst_device, const void* src_host, size_t bytes);
 int xtensor_download(void* dst_host, const void* src_device, size_t bytes);

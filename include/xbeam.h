@@ -73,6 +73,41 @@ int xbeam_logprobs(const void* logits, int dtype, int64_t row_stride, int rows, 
                    int top_k, float* token_lp, float* top_lp, int32_t* top_tok, float* lse, float* entropy, void* stream);
 size_t xbeam_logprobs_workspace_bytes(int rows, int vocab, int top_k);
 
+/*
+ * Verification of drafted tokens (speculative decoding: section 4.4.1's m + 1 query tokens are checked with one pass of the model).  A
+ * sequence's q_len rows of target logits are the model's behind its last token and behind each of its drafts; row t judges draft t, and the
+ * row behind the last draft that stands gives a token of its own.  With p_t = softmax(scale * target row t) and q_t =
+ * softmax(draft_scale * draft row t), what the drafts were drawn from:
+ *     draft x_t stands if all before it do and u[t] * q_t(x_t) < p_t(x_t)
+ *     new token: where draft t falls, from w = max(0, p_t - q_t); where none falls, from w = p behind the last draft
+ *                the least i with sum_{j <= i} w_j > u[q_len - 1] * sum_j w_j
+ * so that the tokens given are distributed as the target's alone, whatever the drafts.  Without draft logits (draft NULL: drafts looked up
+ * in a text, say) q_t is 1 at x_t.  With XBEAM_GREEDY a draft stands if it is the first of row t's largest logits, which is the new token too.
+ *
+ * target       DEVICE [batch * q_len, >= vocab] of `dtype`, rows target_stride values apart (any stride from vocab on), aligned to their type
+ * draft        DEVICE [batch * (q_len - 1), >= vocab] of `dtype`, rows draft_stride apart, or NULL.  Not looked at with XBEAM_GREEDY.
+ * dtype        XBEAM_BF16, XBEAM_FP16 or XBEAM_FP32
+ * scale, draft_scale  positive, 2^-20 to 2^20 (one over a temperature; draft_scale counts with draft logits only)
+ * draft_tokens DEVICE int32 [batch, q_len - 1]; may be NULL with q_len 1.  A token below 0 or from vocab on falls.
+ * n_drafts     DEVICE int32 [batch], how many drafts each sequence has (cut to 0 .. q_len - 1), or NULL: q_len - 1.  Rows behind them are not read.
+ * uniforms     DEVICE fp32 [batch, q_len], in [0, 1): one for each draft, the last for the new token; may be NULL with XBEAM_GREEDY
+ * tokens       DEVICE int32 [batch, q_len]: the drafts that stand, the new token, then -1
+ * n_accepted   DEVICE int32 [batch]: drafts that stand; a sequence keeps kv_len - (q_len - 1 - n_accepted) rows of its cache
+ * token_lp     DEVICE fp32 [batch, q_len] or NULL: ln p of every token given, 0 behind them
+ * Logits of -inf are forbidden tokens.  A target row with +inf or NaN, or of nothing but -inf, has no probabilities: its draft falls, and the new
+ * token is -1 (token_lp NaN).  At a draft row without probabilities the draft falls and w = p.  Where rounding alone let a draft fall, p being
+ * nowhere above q, w = p.
+ * Numerics: whether a draft stands is decided with sums in 32 bits (p and q off by 2^-20 of them at most); the new token's sums are kept in 64
+ * bits, since the borders between tokens lie closer together than 32 bits tell.  Every call with the same inputs gives the same bits.
+ * batch 1..4096, q_len 1..16, vocab 1..2^24.  Asynchronous on `stream`, which it may be captured on; takes the stream's workspace
+ * (xattn_set_workspace; xbeam_verify_workspace_bytes: what one call needs of it), with the rules that xattn_decode states.
+ */
+enum { XBEAM_GREEDY = 1 };
+int xbeam_verify(const void* target, int64_t target_stride, const void* draft, int64_t draft_stride, int dtype, int vocab, float scale,
+                 float draft_scale, const int32_t* draft_tokens, const int32_t* n_drafts, const float* uniforms, int batch, int q_len,
+                 int flags, int32_t* tokens, int32_t* n_accepted, float* token_lp, void* stream);
+size_t xbeam_verify_workspace_bytes(int batch, int q_len, int vocab);
+
 #ifdef __cplusplus
 }
 #endif

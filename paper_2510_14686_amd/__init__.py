@@ -10,4 +10,6 @@ from .binding import (XTENSOR_PAGE_ALLOCATED, XTENSOR_PAGE_FREE, XTENSOR_PAGE_MA
 from .binding import (XATTN_ROPE_DEALT, XATTN_ROPE_PAIRS, XBEAM_BF16, XBEAM_CHECK_INPUT, XBEAM_FP16, XBEAM_FP32, XBEAM_FULL_SORT,  # noqa: F401
                       xattn_prefill, xattn_prefill_workspace_bytes, xattn_rope_kvcache, xbeam_logprobs, xbeam_logprobs_workspace_bytes,
                       xbeam_select)
+from .binding import (XATTN_MX_TILE_BYTES, XATTN_MX_TILE_TOKENS, XBEAM_GREEDY, xattn_decode_mx, xattn_decode_mx_workspace_bytes,  # noqa: F401
+                      xattn_mx_range_bytes, xattn_read_kvcache_mx, xattn_rope_kvcache_mx, xbeam_verify, xbeam_verify_workspace_bytes)
 from .kvstore import KVStore  # noqa: F401

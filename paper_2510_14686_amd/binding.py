@@ -26,9 +26,13 @@ EXPORTS = ["xattn_last_error", "xattn_decode", "xattn_decode_noalloc", "xattn_wo
            "xtensor_pool_create", "xtensor_pool_destroy", "xtensor_pool_counts", "xtensor_page_info",
            "xtensor_open", "xtensor_grow", "xtensor_premap_async", "xtensor_premap_wait", "xtensor_close",
            "xtensor_range_pages", "xattn_write_kvcache", "xattn_mla_decode", "xattn_mla_workspace_bytes", "xbeam_select",
-           "xattn_prefill", "xattn_prefill_workspace_bytes", "xattn_rope_kvcache", "xbeam_logprobs", "xbeam_logprobs_workspace_bytes"]
+           "xattn_prefill", "xattn_prefill_workspace_bytes", "xattn_rope_kvcache", "xbeam_logprobs", "xbeam_logprobs_workspace_bytes",
+           "xattn_mx_range_bytes", "xattn_decode_mx", "xattn_decode_mx_workspace_bytes", "xattn_rope_kvcache_mx", "xattn_read_kvcache_mx", "xbeam_verify",
+           "xbeam_verify_workspace_bytes"]
 XBEAM_FULL_SORT, XBEAM_CHECK_INPUT = 1, 2
 XBEAM_BF16, XBEAM_FP16, XBEAM_FP32 = 0, 1, 2
+XBEAM_GREEDY = 1
+XATTN_MX_TILE_TOKENS, XATTN_MX_TILE_BYTES = 64, 4352
 XATTN_ROPE_PAIRS, XATTN_ROPE_DEALT = 1, 2
 XTENSOR_PAGE_FREE, XTENSOR_PAGE_ALLOCATED, XTENSOR_PAGE_MAPPED, XTENSOR_PAGE_REUSABLE = 0, 1, 2, 3
 
@@ -78,6 +82,13 @@ def _signatures():
         "xattn_rope_kvcache": (i32, [vp, vp, vp, i64, i64, i64, vp, vp, P(i32), i32, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]),
         "xbeam_logprobs": (i32, [vp, i32, i64, i32, i32, f32, vp, i32, vp, vp, vp, vp, vp, vp]),
         "xbeam_logprobs_workspace_bytes": (sz, [i32] * 3),
+        "xattn_mx_range_bytes": (sz, [i64, i32, i32]),
+        "xattn_decode_mx": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, i32, f32, vp, vp, vp]),
+        "xattn_decode_mx_workspace_bytes": (sz, [i32] * 5),
+        "xattn_rope_kvcache_mx": (i32, [vp, vp, vp, i64, i64, i64, vp, vp, P(i32), i32, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, vp, vp]),
+        "xattn_read_kvcache_mx": (i32, [vp, vp, vp, vp, i32, i32, i32, i32, vp, vp, vp]),
+        "xbeam_verify": (i32, [vp, i64, vp, i64, i32, i32, f32, f32, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp]),
+        "xbeam_verify_workspace_bytes": (sz, [i32] * 3),
     }
 
 
@@ -368,6 +379,76 @@ def xbeam_logprobs(logits, dtype: int, row_stride: int, rows: int, vocab: int, s
 
 def xbeam_logprobs_workspace_bytes(rows: int, vocab: int, top_k: int) -> int:
     n = int(load_library().xbeam_logprobs_workspace_bytes(rows, vocab, top_k))
+    if n == 0:
+        raise XattnError(XATTN_EUNSUPPORTED, xattn_last_error())
+    return n
+
+
+def xattn_mx_range_bytes(tokens: int, n_kv_heads: int, head_dim: int = 128) -> int:
+    """Bytes of a K or V range of so many tokens in a cache of 4 bits a value: whole tiles."""
+    n = int(load_library().xattn_mx_range_bytes(tokens, n_kv_heads, head_dim))
+    if n == 0 and tokens != 0:
+        raise XattnError(XATTN_EUNSUPPORTED, xattn_last_error())
+    return n
+
+
+def xattn_decode_mx(q, k_ptrs, v_ptrs, kv_lens, batch: int, q_len: int, n_q_heads: int, n_kv_heads: int, head_dim: int, scale: float, out,
+                    lse=None, stream=None) -> None:
+    """Enqueue decode attention over a cache of 4 bits a value; see include/xattn.h."""
+    if stream is not None and not isinstance(stream, int):
+        stream = int(stream.cuda_stream)
+    status = (_lib or load_library()).xattn_decode_mx(_ptr(q), _ptr(k_ptrs), _ptr(v_ptrs), _ptr(kv_lens), batch, q_len, n_q_heads, n_kv_heads, head_dim,
+                                                      scale if type(scale) is float else ctypes.c_float(scale), _ptr(out), _ptr(lse), stream)
+    if status < 0:
+        _check(status)
+
+
+def xattn_decode_mx_workspace_bytes(batch: int, q_len: int, n_q_heads: int, n_kv_heads: int, head_dim: int = 128) -> int:
+    n = int(load_library().xattn_decode_mx_workspace_bytes(batch, q_len, n_q_heads, n_kv_heads, head_dim))
+    if n == 0:
+        raise XattnError(XATTN_EUNSUPPORTED, xattn_last_error())
+    return n
+
+
+def xattn_rope_kvcache_mx(q, k_new, v_new, q_stride: int, k_stride: int, v_stride: int, pos, inv_freq, sections, flags: int, k_ptrs, v_ptrs,
+                          q_starts, kv_lens, batch: int, total_q: int, n_q_heads: int, n_kv_heads: int, head_dim: int, q_out, stream=None) -> None:
+    """xattn_rope_kvcache into a cache of 4 bits a value; see include/xattn.h."""
+    if stream is not None and not isinstance(stream, int):
+        stream = int(stream.cuda_stream)
+    status = (_lib or load_library()).xattn_rope_kvcache_mx(_ptr(q), _ptr(k_new), _ptr(v_new), q_stride, k_stride, v_stride, _ptr(pos), _ptr(inv_freq),
+                                                            _sections_array(sections), len(sections), flags, _ptr(k_ptrs), _ptr(v_ptrs),
+                                                            _ptr(q_starts), _ptr(kv_lens), batch, total_q, n_q_heads, n_kv_heads, head_dim,
+                                                            _ptr(q_out), stream)
+    if status < 0:
+        _check(status)
+
+
+def xattn_read_kvcache_mx(k_ptrs, v_ptrs, q_starts, kv_lens, batch: int, total_q: int, n_kv_heads: int, head_dim: int, k_out, v_out, stream=None) -> None:
+    """Enqueue the reading of rows of a cache of 4 bits a value, as bf16; see include/xattn.h."""
+    if stream is not None and not isinstance(stream, int):
+        stream = int(stream.cuda_stream)
+    status = (_lib or load_library()).xattn_read_kvcache_mx(_ptr(k_ptrs), _ptr(v_ptrs), _ptr(q_starts), _ptr(kv_lens), batch, total_q, n_kv_heads, head_dim,
+                                                            _ptr(k_out), _ptr(v_out), stream)
+    if status < 0:
+        _check(status)
+
+
+def xbeam_verify(target, target_stride: int, draft, draft_stride: int, dtype: int, vocab: int, scale: float, draft_scale: float, draft_tokens,
+                 n_drafts, uniforms, batch: int, q_len: int, flags: int, tokens, n_accepted, token_lp=None, stream=None) -> None:
+    """Enqueue the verification of drafted tokens; see include/xbeam.h.  All pointers are device addresses; strides in values."""
+    if stream is not None and not isinstance(stream, int):
+        stream = int(stream.cuda_stream)
+    status = (_lib or load_library()).xbeam_verify(_ptr(target), target_stride, _ptr(draft), draft_stride, dtype, vocab,
+                                                   scale if type(scale) is float else ctypes.c_float(scale),
+                                                   draft_scale if type(draft_scale) is float else ctypes.c_float(draft_scale), _ptr(draft_tokens),
+                                                   _ptr(n_drafts), _ptr(uniforms), batch, q_len, flags, _ptr(tokens), _ptr(n_accepted),
+                                                   _ptr(token_lp), stream)
+    if status < 0:
+        _check(status)
+
+
+def xbeam_verify_workspace_bytes(batch: int, q_len: int, vocab: int) -> int:
+    n = int(load_library().xbeam_verify_workspace_bytes(batch, q_len, vocab))
     if n == 0:
         raise XattnError(XATTN_EUNSUPPORTED, xattn_last_error())
     return n

@@ -61,18 +61,13 @@ int g_timed_calls = 0;
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-struct WorkspaceLayout {
-    size_t meta_off, ml_off, o_off, total;
-};
-WorkspaceLayout layout_for(int batch, int q_len, int n_q_heads, int n_pieces);
-
 // How a GQA call's keys are cut on the vector path: the number of pieces, and how many of them a workgroup holds.
 struct DecodeSplit {
     int pieces, parts;
 };
 // What every GQA call needs of workspace: one piece per compute unit (or the configured pieces).
 size_t decode_least_bytes(int n_cu, int batch, int q_len, int n_q_heads) {
-    return layout_for(batch, q_len, n_q_heads, g_cfg_pieces > 0 ? g_cfg_pieces : n_cu).total;
+    return decode_layout(batch, q_len, n_q_heads, g_cfg_pieces > 0 ? g_cfg_pieces : n_cu).total;
 }
 // One workgroup per compute unit.  A wave of the vector path streams one KV head, so with fewer than eight KV heads a
 // workgroup takes several pieces to keep eight waves' loads in flight (two KV heads, 138468 tokens: 46.6 us
@@ -90,7 +85,7 @@ DecodeSplit decode_split(int n_cu, int batch, int q_len, int n_q_heads, int n_kv
     const int pieces = groups == 1 ? n_cu : shared < 8 ? 8 : shared;
     if (have > XATTN_NOALLOC_SCRATCH_BYTES) have = XATTN_NOALLOC_SCRATCH_BYTES;
     int parts = most;
-    while (parts > 1 && layout_for(batch, q_len, n_q_heads, pieces * parts).total > have) --parts;
+    while (parts > 1 && decode_layout(batch, q_len, n_q_heads, pieces * parts).total > have) --parts;
     return DecodeSplit{pieces * parts, parts};
 }
 
@@ -111,17 +106,6 @@ int mla_pieces_for(int n_cu, int q_len, int n_heads) {
     const int n_groups = (q_len * n_heads + rows_per_group - 1) / rows_per_group;
     const int pieces = n_cu / n_groups / 8 * 8;
     return pieces < 8 ? 8 : pieces;
-}
-
-WorkspaceLayout layout_for(int batch, int q_len, int n_q_heads, int n_pieces) {
-    const size_t slots = (size_t)n_pieces + (size_t)batch;
-    const size_t rows = (size_t)q_len * (size_t)n_q_heads;
-    WorkspaceLayout w;
-    w.meta_off = 0;
-    w.ml_off = align_up((size_t)batch * 2 * sizeof(int32_t), 256);
-    w.o_off = w.ml_off + align_up(slots * rows * 2 * sizeof(float), 256);
-    w.total = w.o_off + align_up(slots * rows * kHeadDim * sizeof(float), 256);
-    return w;
 }
 
 // Latent-KV call: per-sequence table, (m, l, lq, 1 / scale) per partial row, partial rows of 512 fp16.
@@ -146,20 +130,6 @@ int check_mla_shape(int batch, int q_len, int n_heads, int d_latent, int d_rope)
     if (batch > kMaxBatch) return fail(XATTN_EUNSUPPORTED, "batch %d exceeds %d", batch, kMaxBatch);
     if (q_len > kMaxQLen) return fail(XATTN_EUNSUPPORTED, "q_len %d exceeds %d", q_len, kMaxQLen);
     if ((long)q_len * n_heads > 4096) return fail(XATTN_EUNSUPPORTED, "q_len * n_heads = %ld exceeds 4096", (long)q_len * n_heads);
-    return XATTN_OK;
-}
-
-int check_shape(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim) {
-    if (batch < 1 || q_len < 1 || n_q_heads < 1 || n_kv_heads < 1 || head_dim < 1)
-        return fail(XATTN_EINVAL, "batch, q_len, n_q_heads, n_kv_heads and head_dim must be positive");
-    if (n_q_heads % n_kv_heads != 0)
-        return fail(XATTN_EUNSUPPORTED, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", n_q_heads, n_kv_heads);
-    if (head_dim != kHeadDim) return fail(XATTN_EUNSUPPORTED, "head_dim %d: only 128 is supported", head_dim);
-    if (batch > kMaxBatch) return fail(XATTN_EUNSUPPORTED, "batch %d exceeds %d", batch, kMaxBatch);
-    if (q_len > kMaxQLen) return fail(XATTN_EUNSUPPORTED, "q_len %d exceeds %d", q_len, kMaxQLen);
-    if ((n_q_heads / n_kv_heads) * q_len > kMaxRows)
-        return fail(XATTN_EUNSUPPORTED, "(n_q_heads / n_kv_heads) * q_len = %d exceeds %d",
-                    (n_q_heads / n_kv_heads) * q_len, kMaxRows);
     return XATTN_OK;
 }
 
@@ -247,6 +217,31 @@ int timing_events(hipEvent_t** events_out) {
 
 }  // namespace
 
+DecodeLayout decode_layout(int batch, int q_len, int n_q_heads, int n_pieces) {
+    const size_t slots = (size_t)n_pieces + (size_t)batch;
+    const size_t rows = (size_t)q_len * (size_t)n_q_heads;
+    DecodeLayout w;
+    w.meta_off = 0;
+    w.ml_off = align_up((size_t)batch * 2 * sizeof(int32_t), 256);
+    w.o_off = w.ml_off + align_up(slots * rows * 2 * sizeof(float), 256);
+    w.total = w.o_off + align_up(slots * rows * kHeadDim * sizeof(float), 256);
+    return w;
+}
+
+int check_decode_shape(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim) {
+    if (batch < 1 || q_len < 1 || n_q_heads < 1 || n_kv_heads < 1 || head_dim < 1)
+        return fail(XATTN_EINVAL, "batch, q_len, n_q_heads, n_kv_heads and head_dim must be positive");
+    if (n_q_heads % n_kv_heads != 0)
+        return fail(XATTN_EUNSUPPORTED, "n_q_heads (%d) is not a multiple of n_kv_heads (%d)", n_q_heads, n_kv_heads);
+    if (head_dim != kHeadDim) return fail(XATTN_EUNSUPPORTED, "head_dim %d: only 128 is supported", head_dim);
+    if (batch > kMaxBatch) return fail(XATTN_EUNSUPPORTED, "batch %d exceeds %d", batch, kMaxBatch);
+    if (q_len > kMaxQLen) return fail(XATTN_EUNSUPPORTED, "q_len %d exceeds %d", q_len, kMaxQLen);
+    if ((n_q_heads / n_kv_heads) * q_len > kMaxRows)
+        return fail(XATTN_EUNSUPPORTED, "(n_q_heads / n_kv_heads) * q_len = %d exceeds %d",
+                    (n_q_heads / n_kv_heads) * q_len, kMaxRows);
+    return XATTN_OK;
+}
+
 int with_workspace(const char* who, size_t bytes, void* stream, WorkspaceLaunchFn launch, void* context) {
     std::lock_guard<std::mutex> lock(g_mutex);
     DeviceState* d = nullptr;
@@ -267,7 +262,7 @@ int decode_call(const char* who, FixedWorkspaceFn fixed_workspace, const void* q
                 int n_kv_heads, int head_dim, float scale, void* out, float* lse, void* stream) {
     if (!q || !k_ptrs || !v_ptrs || !kv_lens || !out)
         return fail(XATTN_EINVAL, "%s: q, k_ptrs, v_ptrs, kv_lens and out must not be NULL", who);
-    int st = check_shape(batch, q_len, n_q_heads, n_kv_heads, head_dim);
+    int st = check_decode_shape(batch, q_len, n_q_heads, n_kv_heads, head_dim);
     if (st != XATTN_OK) return st;
     if (!std::isfinite(scale)) return fail(XATTN_EINVAL, "%s: scale is not finite", who);
     if (reinterpret_cast<uintptr_t>(q) % 16 != 0 || reinterpret_cast<uintptr_t>(out) % 16 != 0)
@@ -286,7 +281,7 @@ int decode_call(const char* who, FixedWorkspaceFn fixed_workspace, const void* q
                          : acquire_workspace(d, least, static_cast<hipStream_t>(stream), who, &ws, &have);
     if (st != XATTN_OK) return st;
     const DecodeSplit split = decode_split(d->n_cu, batch, q_len, n_q_heads, n_kv_heads, have);
-    const WorkspaceLayout w = layout_for(batch, q_len, n_q_heads, split.pieces);
+    const DecodeLayout w = decode_layout(batch, q_len, n_q_heads, split.pieces);
 
     DecodeParams prm;
     prm.q = static_cast<const uint16_t*>(q);
@@ -375,12 +370,12 @@ int xattn_configure(int key, int value) {
 }
 
 size_t xattn_workspace_bytes(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim) {
-    if (check_shape(batch, q_len, n_q_heads, n_kv_heads, head_dim) != XATTN_OK) return 0;
+    if (check_decode_shape(batch, q_len, n_q_heads, n_kv_heads, head_dim) != XATTN_OK) return 0;
     // Upper bound over the automatic piece count of any supported device and the configured one.
     DeviceState* d = nullptr;
     const int n_cu = g_cfg_pieces == 0 && device_state(&d, nullptr) == XATTN_OK ? d->n_cu : 256;
     const size_t least = decode_least_bytes(n_cu, batch, q_len, n_q_heads);
-    const size_t split = layout_for(batch, q_len, n_q_heads, decode_split(n_cu, batch, q_len, n_q_heads, n_kv_heads, SIZE_MAX).pieces).total;
+    const size_t split = decode_layout(batch, q_len, n_q_heads, decode_split(n_cu, batch, q_len, n_q_heads, n_kv_heads, SIZE_MAX).pieces).total;
     return split > least ? split : least;
 }
 

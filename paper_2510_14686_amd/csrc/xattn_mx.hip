@@ -1,0 +1,328 @@
+// Split-KV decode attention over a cache of 4 bits a value (xattn_decode_mx; the cache: xattn_mx.h).
+//
+//   s_j = scale <q, k_j>;  out = sum_j softmax(s)_j v_j;  lse = ln sum_j exp(s_j)      with k_j = 2^e code, v_j likewise, per block of 32 values
+//
+// The stream of keys is cut as xattn_decode's is, in whole tiles: a workgroup takes a piece of it for one KV head, its eight waves a
+// run of tiles each; a sequence that the waves cut among themselves is put together in LDS, one that pieces cut by the merge kernel.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <type_traits>
+
+#include "xattn_device.h"
+#include "xattn_launch.h"
+#include "xattn_matrix.h"
+#include "xattn_mx.h"
+
+namespace xattn {
+namespace {
+
+struct TileUnit {
+    static __device__ __forceinline__ int positions(int raw) { return mx_positions(raw); }
+    static __device__ __forceinline__ int stream(int raw, int seg_cost) { return raw > 0 ? mx_positions(raw) + seg_cost : 0; }
+};
+
+// Fixed work of a (piece, sequence) segment, in positions.
+constexpr int kMxSegCost = kMxPositions;
+
+// Lane (kb, n) = (lane / 16, lane % 16) of a tile: K's block kb of tokens 16 s + n; V's values 8 n .. 8 n + 7 of tokens 16 s + 4 kb + r.
+struct MxTile {
+    u32x4_t k[4], v[4], vs;
+    uint32_t ks;
+};
+__device__ __forceinline__ void load_tile(MxTile& t, const char* kt, const char* vt, int lane) {
+    const int kb = lane >> 4, n = lane & 15;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) t.k[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kt + lane * 16 + 1024 * s));
+    t.ks = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(kt + kMxCodeBytes + lane * 4));
+#pragma unroll
+    for (int s = 0; s < 4; ++s) t.v[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vt + lane * 16 + 1024 * s));
+    t.vs = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vt + kMxCodeBytes + (4 * kb + (n >> 2)) * 16));
+}
+
+// The scale in byte i of four as a float.
+__device__ __forceinline__ float scale_of(uint32_t bytes, int i) { return __uint_as_float((i == 3 ? bytes >> 1 : bytes << (23 - 8 * i)) & 0x7f800000u); }
+// The codes in byte i of four, times the scale, as two bf16: exact.
+template <int kByte>
+__device__ __forceinline__ uint32_t unpack(uint32_t codes, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, kByte));
+}
+
+// One tile against kTiles times 16 query rows.  s[t][i][j] is the score of key 16 i + 4 kb + j for row n: a lane holds keys of one row, and the
+// products of these with V take them from where they are.
+template <int kTiles>
+__device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], MxTile& r, const bf16x8_t (&qop)[kTiles][4], float scale_log2, int key0, int L,
+                                        const int (&lim)[kTiles], int kb) {
+    f32x4_t s[kTiles][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float scale = scale_of(r.ks, i);
+#pragma unroll
+        for (int t = 0; t < kTiles; ++t) s[t][i] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int step = 0; step < 4; ++step) {
+            const uint32_t w = r.k[i][step];
+            const u32x4_t a = {unpack<0>(w, scale), unpack<1>(w, scale), unpack<2>(w, scale), unpack<3>(w, scale)};
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), qop[t][step], s[t][i], 0, 0, 0);
+        }
+    }
+    u32x4_t hi[kTiles][2], lo[kTiles][2];
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[t][i] *= scale_log2;
+        if (__builtin_amdgcn_ballot_w64(key0 + kMxTileTokens > lim[t]) != 0) {      // only tiles that reach a limit
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[t][i][j] = key0 + 16 * i + 4 * kb + j < lim[t] ? s[t][i][j] : kNegInf;
+        }
+        float mx = kNegInf;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(fmaxf(s[t][i][0], s[t][i][1]), fmaxf(s[t][i][2], s[t][i][3])));
+        mx = kb_max(mx);
+        const bool moves = mx > st[t].m;
+        if (__builtin_amdgcn_ballot_w64(moves) != 0) {
+            const float m_new = moves ? mx : st[t].m;
+            const float alpha = moves ? fast_exp2(st[t].m - m_new) : 1.0f;
+            st[t].m = m_new;
+            st[t].l *= alpha;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) st[t].o[e] *= alpha;
+        }
+        const float m_use = st[t].m == kNegInf ? 0.0f : st[t].m;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[t][i][j] = fast_exp2(s[t][i][j] - m_use);
+            st[t].l += (s[t][i][0] + s[t][i][1]) + (s[t][i][2] + s[t][i][3]);
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                const f32x2_t p = {s[t][i][j], s[t][i][j + 1]};
+                const bf16x2_t h = __builtin_convertvector(p, bf16x2_t);
+                const f32x2_t rest = p - __builtin_convertvector(h, f32x2_t);
+                hi[t][i >> 1][(i & 1) * 2 + (j >> 1)] = __builtin_bit_cast(uint32_t, h);
+                lo[t][i >> 1][(i & 1) * 2 + (j >> 1)] = cvt_bf16(rest[0], rest[1]);
+            }
+        }
+    }
+    // What stands behind the sequence's last key may be anything: its weight is 0, and with a scale of 2^-127 so is the product.
+    if (key0 + kMxTileTokens > L) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int left = L - (key0 + 16 * i + 4 * kb);
+            r.vs[i] &= left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1;
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t x[8][4];      // token 4 i + r: pairs of values
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const float scale = scale_of(r.vs[2 * h + i], q);
+                const uint32_t w = r.v[2 * h + i][q];
+                x[4 * i + q][0] = unpack<0>(w, scale);
+                x[4 * i + q][1] = unpack<1>(w, scale);
+                x[4 * i + q][2] = unpack<2>(w, scale);
+                x[4 * i + q][3] = unpack<3>(w, scale);
+            }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;      // high or low halves of both words
+            u32x4_t a;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(x[2 * i + 1][e >> 1], x[2 * i][e >> 1], sel);
+#pragma unroll
+            for (int t = 0; t < kTiles; ++t) {
+                st[t].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, hi[t][h]), st[t].o[e], 0, 0, 0);
+                st[t].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, lo[t][h]), st[t].o[e], 0, 0, 0);
+            }
+        }
+    }
+}
+
+// A segment in flight: its Q operand, its limits and its first tile.  seg.j0 and j1 are positions of the stream, seg.L tokens.
+template <int kTiles>
+struct MxCtx {
+    Segment seg;
+    const char* kp;      // the segment's first tile
+    const char* vp;
+    bf16x8_t qop[kTiles][4];
+    int lim[kTiles];     // first key that row n of the tile may not see
+    MxTile first;
+};
+template <int kTiles>
+__device__ __forceinline__ void mx_begin(MxCtx<kTiles>& c, const DecodeParams& prm, const Segment& seg, int lane) {
+    const int kb = lane >> 4, n = lane & 15;
+    c.seg = seg;
+    const int64_t at = ((int64_t)(seg.j0 / kMxPositions) * prm.n_kv_heads + seg.kvh) * kMxTileBytes;
+    c.kp = static_cast<const char*>(seg.kp) + at;
+    c.vp = static_cast<const char*>(seg.vp) + at;
+    load_tile(c.first, c.kp, c.vp, lane);
+    // Q through a descriptor over the sequence's rows: rows past n_rows lie past its end and read as zero.
+    const int seq_rows = prm.q_len * prm.n_q_heads;
+    const __amdgpu_buffer_rsrc_t rq = make_rsrc(prm.q + (long)seg.b * seq_rows * kHeadDim, (uint32_t)(seq_rows * kRowBytes));
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+        const bool row_ok = 16 * t + n < seg.n_rows;
+        const int r = row_ok ? 16 * t + n : 0;
+        const int qoff = (row_ok ? seq_row(prm, seg, r) : seq_rows) * kRowBytes + kb * 64;
+#pragma unroll
+        for (int step = 0; step < 4; ++step)
+            c.qop[t][step] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rq, qoff + 16 * step, 0, 0));
+        c.lim[t] = seg.L - prm.q_len + row_token(prm, seg.row0 + r) + 1;
+    }
+}
+
+template <int kTiles>
+__device__ __forceinline__ void mx_run(MatrixState (&st)[kTiles], MxCtx<kTiles>& c, const DecodeParams& prm, int lane) {
+    const int kb = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) st[t].o[e] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        st[t].m = kNegInf;
+        st[t].l = 0.0f;
+    }
+    const int64_t step = (int64_t)prm.n_kv_heads * kMxTileBytes;
+    const int first = c.seg.j0 / kMxPositions, n_tiles = c.seg.j1 / kMxPositions - first;
+    MxTile other;
+    int i = 0;
+    for (; i + 2 <= n_tiles; i += 2) {
+        load_tile(other, c.kp + (i + 1) * step, c.vp + (i + 1) * step, lane);
+        mx_tile<kTiles>(st, c.first, c.qop, prm.scale_log2, (first + i) * kMxTileTokens, c.seg.L, c.lim, kb);
+        if (i + 2 < n_tiles) load_tile(c.first, c.kp + (i + 2) * step, c.vp + (i + 2) * step, lane);
+        mx_tile<kTiles>(st, other, c.qop, prm.scale_log2, (first + i + 1) * kMxTileTokens, c.seg.L, c.lim, kb);
+    }
+    if (i < n_tiles) mx_tile<kTiles>(st, c.first, c.qop, prm.scale_log2, (first + i) * kMxTileTokens, c.seg.L, c.lim, kb);
+}
+
+// grid.x = workgroups of pieces times groups of R query rows, grid.z = KV heads.  (What the plan needs are arguments of their own: see
+// split_decode_kernel, whose walk over a piece this one shares.)
+template <int R>
+__global__ __launch_bounds__(64 * kMxWaves) void decode_mx_kernel(const int32_t* __restrict__ kv_lens, const void* const* k_ptrs, const void* const* v_ptrs,
+                                                                 int batch, int n_pieces, int min_piece, int few_pieces, int few_min,
+                                                                 int xcd_skew, int grid_x, DecodeParams prm) {
+    constexpr int kTiles = R / 16;
+    constexpr int kStates = (kMxWaves - 1) * kTiles;
+    __shared__ __attribute__((aligned(16))) char lds[kMxWaves * kLdsPerWave + kStates * kLdsPerState];
+    const int lane = threadIdx.x & 63;
+    const int part = uniform((int)(threadIdx.x >> 6));
+    SeqWindow win;
+    const WavePlan wp = wave_plan<TileUnit>(kv_lens, k_ptrs, v_ptrs, batch, n_pieces, min_piece, kMxSegCost, xcd_skew, FewPieces{few_pieces, few_min}, lane,
+                                            &win, kMxWaves);
+    const Plan& pl = wp.pl;
+    const int bid = blockIdx.x, rows_total = prm.group * prm.q_len;
+    const DecodeWork work = decode_work(pl, grid_x, 1, rows_total, R, bid, 0);
+    const int p = work.piece, rows = work.rows;
+    const int piece0 = piece_bound(pl, p), piece1 = piece_bound(pl, p + 1);
+    const int sub = part_positions(piece1 - piece0, kMxWaves), s0 = piece0 + part * sub, s1 = s0 + sub < piece1 ? s0 + sub : piece1;
+    if (__builtin_expect(64 * (grid_x - 1 - bid) < batch && blockIdx.z == 0 && part == kMxWaves - 1, 0)) {
+        for (int g = grid_x - 1 - bid; 64 * g < batch; g += grid_x)
+            wave_write_meta<TileUnit>(wp, kv_lens, batch, prm.q_len * prm.n_q_heads, g, lane, prm.meta);
+    }
+    if (!work.any || piece0 >= piece1) return;      // the whole workgroup
+    const bool active = s0 < s1;
+    Walk walk;
+    if (active) wave_locate<TileUnit>(wp, kv_lens, k_ptrs, v_ptrs, batch, s0, lane, &win, walk.b, walk.j);
+    walk.remaining = uniform(s1 - s0);
+
+    Segment seg;
+    seg.kvh = blockIdx.z;
+    seg.row0 = work.row0;
+    seg.n_rows = rows_total - seg.row0 < rows ? rows_total - seg.row0 : rows;
+    // The next (piece, sequence) intersection, in stream order; false when the piece is done.
+    auto next_seg = [&](Segment& out, int& positions, auto first) {
+        constexpr bool kFirst = decltype(first)::value;
+        PieceSeg ps;
+        int tokens = 0;
+        auto len_of = [&](int b) {
+            if constexpr (kFirst) tokens = window_len(win, kv_lens, b);
+            else tokens = uniform(clamp_len(kv_lens[b]));
+            return mx_positions(tokens);
+        };
+        if (!next_segment(walk, batch, pl.seg_cost, len_of, ps)) return false;
+        out = seg;
+        out.b = uniform(ps.b);
+        out.kp = kFirst ? window_ptr(win, win.k, k_ptrs, out.b) : uniform(k_ptrs[out.b]);
+        out.vp = kFirst ? window_ptr(win, win.v, v_ptrs, out.b) : uniform(v_ptrs[out.b]);
+        out.L = uniform(tokens);
+        out.j0 = uniform(ps.j0);
+        out.j1 = uniform(ps.j1);
+        out.slot = uniform(p) + out.b;
+        out.whole = uniform(ps.whole);
+        positions = uniform(ps.L);
+        return true;
+    };
+    char* const lds_wave = lds + part * kLdsPerWave;
+    auto run_piece = [&](auto tiles) {
+        constexpr int kT = decltype(tiles)::value;
+        auto state_of = [&](int of_part, int t) { return lds + kMxWaves * kLdsPerWave + ((of_part - 1) * kT + t) * kLdsPerState; };
+        MatrixState st[kT];
+        MxCtx<kT> cur;
+        int positions = 0;
+        auto put = [&] {
+#pragma unroll
+            for (int t = 0; t < kT; ++t) state_put(st[t], state_of(part, t), lane);
+        };
+        bool have = false;
+        if (active) {
+            Segment first;
+            have = uniform(next_seg(first, positions, std::true_type())) != 0;
+            if (have) mx_begin(cur, prm, first, lane);
+        }
+        if (have) {
+            for (;;) {
+                mx_run<kT>(st, cur, prm, lane);
+                Segment nxt_seg;
+                int nxt_positions;
+                if (uniform(next_seg(nxt_seg, nxt_positions, std::false_type())) == 0) break;
+                MxCtx<kT> nxt;
+                mx_begin(nxt, prm, nxt_seg, lane);     // its loads go out before cur's stores
+                if (part > 0 && cur.seg.j0 > 0) {
+                    put();
+                } else {
+#pragma unroll
+                    for (int t = 0; t < kT; ++t) matrix_finish<true>(st[t], cur.seg, t, prm, lane, lds_wave);
+                }
+                cur = nxt;
+                positions = nxt_positions;
+            }
+        }
+        // The last segment: what the wave before began goes to LDS, what this wave begins is put together there.
+        PartRun run = {false, 0, false};
+        if (have) run = part_run(part, cur.seg.j0, cur.seg.j1, positions, piece1 - s1, sub);
+        if (have && run.prev) put();
+        __syncthreads();
+        if (!have || run.prev) return;
+        for (int q = part + 1; q <= part + run.next; ++q)
+#pragma unroll
+            for (int t = 0; t < kT; ++t) state_add(st[t], state_of(q, t), lane);
+        cur.seg.whole = cur.seg.j0 == 0 && run.ends;
+#pragma unroll
+        for (int t = 0; t < kT; ++t) matrix_finish<false>(st[t], cur.seg, t, prm, lane, lds_wave);
+    };
+    if (kTiles == 2 && rows == 16) run_piece(std::integral_constant<int, 1>());
+    else run_piece(std::integral_constant<int, kTiles>());
+}
+
+template <int R>
+hipError_t launch_r(const DecodeParams& prm, hipStream_t stream) {
+    const int grid_x = decode_grid_x(prm.n_pieces, 1, prm.group * prm.q_len, R);
+    return launch(decode_mx_kernel<R>, dim3((unsigned)grid_x, 1, (unsigned)prm.n_kv_heads), 64 * kMxWaves, stream, prm.kv_lens, prm.k_ptrs, prm.v_ptrs, prm.batch,
+                  prm.n_pieces, prm.min_piece_tokens, prm.few.pieces, prm.few.min_piece, prm.xcd_skew, grid_x, prm);
+}
+
+}  // namespace
+
+int mx_rows_per_wave(int rows_total) { return rows_total <= 16 ? 16 : 32; }
+
+hipError_t launch_decode_mx(const DecodeParams& prm, hipStream_t stream) {
+    const hipError_t e = mx_rows_per_wave(prm.group * prm.q_len) == 16 ? launch_r<16>(prm, stream) : launch_r<32>(prm, stream);
+    return e != hipSuccess ? e : launch_decode_merge(prm, stream);
+}
+
+}  // namespace xattn

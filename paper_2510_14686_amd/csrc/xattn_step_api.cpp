@@ -27,21 +27,8 @@ bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p
 
 size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-// What both cache operators ask of a packed batch.
-int check_batch(const char* who, int batch, int total_q, int n_q_heads, int n_kv_heads, int head_dim) {
-    if (batch < 1 || total_q < 1 || n_q_heads < 1 || n_kv_heads < 1 || head_dim < 1)
-        return fail(XATTN_EINVAL, "%s: batch, total_q, n_q_heads, n_kv_heads and head_dim must be positive", who);
-    if (batch > kMaxBatch) return fail(XATTN_EUNSUPPORTED, "%s: batch %d exceeds %d", who, batch, kMaxBatch);
-    if (total_q > kMaxTotalQ) return fail(XATTN_EUNSUPPORTED, "%s: total_q %d exceeds %d", who, total_q, kMaxTotalQ);
-    if (n_q_heads > kMaxHeads || n_kv_heads > kMaxHeads)
-        return fail(XATTN_EUNSUPPORTED, "%s: %d query heads, %d KV heads: more than %d", who, n_q_heads, n_kv_heads, kMaxHeads);
-    if ((long)total_q * n_q_heads > kMaxRowsOfHeads)
-        return fail(XATTN_EUNSUPPORTED, "%s: total_q * n_q_heads = %ld exceeds %d", who, (long)total_q * n_q_heads, kMaxRowsOfHeads);
-    return XATTN_OK;
-}
-
 int check_prefill(const char* who, int batch, int total_q, int n_q_heads, int n_kv_heads, int head_dim) {
-    const int st = check_batch(who, batch, total_q, n_q_heads, n_kv_heads, head_dim);
+    const int st = check_packed_batch(who, batch, total_q, n_q_heads, n_kv_heads, head_dim);
     if (st != XATTN_OK) return st;
     if (n_q_heads % n_kv_heads != 0)
         return fail(XATTN_EUNSUPPORTED, "%s: n_q_heads (%d) is not a multiple of n_kv_heads (%d)", who, n_q_heads, n_kv_heads);
@@ -73,6 +60,83 @@ int check_logprobs(const char* who, int rows, int vocab, int top_k) {
 }
 
 }  // namespace
+
+int check_packed_batch(const char* who, int batch, int total_q, int n_q_heads, int n_kv_heads, int head_dim) {
+    if (batch < 1 || total_q < 1 || n_q_heads < 1 || n_kv_heads < 1 || head_dim < 1)
+        return fail(XATTN_EINVAL, "%s: batch, total_q, n_q_heads, n_kv_heads and head_dim must be positive", who);
+    if (batch > kMaxBatch) return fail(XATTN_EUNSUPPORTED, "%s: batch %d exceeds %d", who, batch, kMaxBatch);
+    if (total_q > kMaxTotalQ) return fail(XATTN_EUNSUPPORTED, "%s: total_q %d exceeds %d", who, total_q, kMaxTotalQ);
+    if (n_q_heads > kMaxHeads || n_kv_heads > kMaxHeads)
+        return fail(XATTN_EUNSUPPORTED, "%s: %d query heads, %d KV heads: more than %d", who, n_q_heads, n_kv_heads, kMaxHeads);
+    if ((long)total_q * n_q_heads > kMaxRowsOfHeads)
+        return fail(XATTN_EUNSUPPORTED, "%s: total_q * n_q_heads = %ld exceeds %d", who, (long)total_q * n_q_heads, kMaxRowsOfHeads);
+    return XATTN_OK;
+}
+
+int make_rope(const char* who, const void* q, const void* k_new, const void* v_new, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+              const int32_t* pos, const float* inv_freq, const int32_t* sections, int n_axes, int flags, void* const* k_ptrs,
+              void* const* v_ptrs, const int32_t* q_starts, const int32_t* kv_lens, int batch, int total_q, int n_q_heads, int n_kv_heads,
+              int head_dim, void* q_out, RopeParams* prm_out) {
+    if (!q || !k_new || !v_new || !pos || !sections || !k_ptrs || !v_ptrs || !q_starts || !kv_lens || !q_out)
+        return fail(XATTN_EINVAL, "%s: NULL argument", who);
+    const int st = check_packed_batch(who, batch, total_q, n_q_heads, n_kv_heads, head_dim);
+    if (st != XATTN_OK) return st;
+    if (flags & ~(XATTN_ROPE_PAIRS | XATTN_ROPE_DEALT)) return fail(XATTN_EINVAL, "%s: unknown flags 0x%x", who, flags);
+    if (head_dim % 16 != 0 || head_dim > kRopeMaxHeadDim)
+        return fail(XATTN_EUNSUPPORTED, "%s: head_dim %d is not a multiple of 16 up to %d", who, head_dim, kRopeMaxHeadDim);
+    if (n_axes < 1 || n_axes > kRopeMaxAxes) return fail(XATTN_EUNSUPPORTED, "%s: %d axes: one to four are supported", who, n_axes);
+    int left[kRopeMaxAxes] = {}, frequencies = 0;
+    for (int a = 0; a < n_axes; ++a) {
+        if (sections[a] < 0 || sections[a] > head_dim / 2)
+            return fail(XATTN_EINVAL, "%s: section %d has %d frequencies of head_dim / 2 = %d", who, a, (int)sections[a], head_dim / 2);
+        left[a] = sections[a];
+        frequencies += sections[a];
+    }
+    if (frequencies > head_dim / 2)
+        return fail(XATTN_EINVAL, "%s: %d frequencies in all, head_dim %d has %d", who, frequencies, head_dim, head_dim / 2);
+    if (frequencies > 0 && !inv_freq) return fail(XATTN_EINVAL, "%s: NULL argument", who);
+    if (frequencies % 8 != 0) return fail(XATTN_EUNSUPPORTED, "%s: %d frequencies in all: a multiple of 8 is supported", who, frequencies);
+    if (q_stride < (int64_t)n_q_heads * head_dim || k_stride < (int64_t)n_kv_heads * head_dim || v_stride < (int64_t)n_kv_heads * head_dim)
+        return fail(XATTN_EINVAL, "%s: a row stride is less than the row's heads * head_dim", who);
+    if (q_stride > (int64_t)1 << 32 || k_stride > (int64_t)1 << 32 || v_stride > (int64_t)1 << 32)
+        return fail(XATTN_EUNSUPPORTED, "%s: a row stride exceeds 2^32 values", who);
+    if (q_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0 || misaligned(q, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) ||
+        misaligned(q_out, 16))
+        return fail(XATTN_EINVAL, "%s: q, k_new, v_new, q_out and the row strides must be multiples of 16 bytes", who);
+
+    if (q_out == q && q_stride != (int64_t)n_q_heads * head_dim)
+        return fail(XATTN_EINVAL, "%s: q_out may be q only where q's rows are contiguous", who);
+
+    RopeParams& prm = *prm_out;
+    prm = RopeParams{};
+    prm.q = static_cast<const uint16_t*>(q);
+    prm.k = static_cast<const uint16_t*>(k_new);
+    prm.v = static_cast<const uint16_t*>(v_new);
+    prm.q_stride = q_stride;
+    prm.k_stride = k_stride;
+    prm.v_stride = v_stride;
+    prm.pos = pos;
+    prm.inv_freq = inv_freq;
+    prm.k_ptrs = k_ptrs;
+    prm.v_ptrs = v_ptrs;
+    prm.q_starts = q_starts;
+    prm.kv_lens = kv_lens;
+    prm.q_out = static_cast<uint16_t*>(q_out);
+    prm.batch = batch;
+    prm.total_q = total_q;
+    prm.n_q_heads = n_q_heads;
+    prm.n_kv_heads = n_kv_heads;
+    prm.head_dim = head_dim;
+    prm.frequencies = frequencies;
+    prm.pairs = flags & XATTN_ROPE_PAIRS ? 1 : 0;
+    for (int i = 0, axis = 0; i < frequencies; ++i) {
+        while (left[axis] == 0) axis = (axis + 1) % n_axes;
+        prm.axis_of[i >> 4] |= (uint32_t)axis << (2 * (i & 15));
+        --left[axis];
+        if (flags & XATTN_ROPE_DEALT) axis = (axis + 1) % n_axes;
+    }
+    return XATTN_OK;
+}
 
 }  // namespace xattn
 
@@ -136,64 +200,10 @@ int xattn_rope_kvcache(const void* q, const void* k_new, const void* v_new, int6
                        const int32_t* pos, const float* inv_freq, const int32_t* sections, int n_axes, int flags,
                        void* const* k_ptrs, void* const* v_ptrs, const int32_t* q_starts, const int32_t* kv_lens, int batch,
                        int total_q, int n_q_heads, int n_kv_heads, int head_dim, void* q_out, void* stream) {
-    const char* const who = "xattn_rope_kvcache";
-    if (!q || !k_new || !v_new || !pos || !sections || !k_ptrs || !v_ptrs || !q_starts || !kv_lens || !q_out)
-        return fail(XATTN_EINVAL, "%s: NULL argument", who);
-    const int st = check_batch(who, batch, total_q, n_q_heads, n_kv_heads, head_dim);
+    RopeParams prm;
+    const int st = make_rope("xattn_rope_kvcache", q, k_new, v_new, q_stride, k_stride, v_stride, pos, inv_freq, sections, n_axes, flags, k_ptrs, v_ptrs,
+                             q_starts, kv_lens, batch, total_q, n_q_heads, n_kv_heads, head_dim, q_out, &prm);
     if (st != XATTN_OK) return st;
-    if (flags & ~(XATTN_ROPE_PAIRS | XATTN_ROPE_DEALT)) return fail(XATTN_EINVAL, "%s: unknown flags 0x%x", who, flags);
-    if (head_dim % 16 != 0 || head_dim > kRopeMaxHeadDim)
-        return fail(XATTN_EUNSUPPORTED, "%s: head_dim %d is not a multiple of 16 up to %d", who, head_dim, kRopeMaxHeadDim);
-    if (n_axes < 1 || n_axes > kRopeMaxAxes) return fail(XATTN_EUNSUPPORTED, "%s: %d axes: one to four are supported", who, n_axes);
-    int left[kRopeMaxAxes] = {}, frequencies = 0;
-    for (int a = 0; a < n_axes; ++a) {
-        if (sections[a] < 0 || sections[a] > head_dim / 2)
-            return fail(XATTN_EINVAL, "%s: section %d has %d frequencies of head_dim / 2 = %d", who, a, (int)sections[a], head_dim / 2);
-        left[a] = sections[a];
-        frequencies += sections[a];
-    }
-    if (frequencies > head_dim / 2)
-        return fail(XATTN_EINVAL, "%s: %d frequencies in all, head_dim %d has %d", who, frequencies, head_dim, head_dim / 2);
-    if (frequencies > 0 && !inv_freq) return fail(XATTN_EINVAL, "%s: NULL argument", who);
-    if (frequencies % 8 != 0) return fail(XATTN_EUNSUPPORTED, "%s: %d frequencies in all: a multiple of 8 is supported", who, frequencies);
-    if (q_stride < (int64_t)n_q_heads * head_dim || k_stride < (int64_t)n_kv_heads * head_dim || v_stride < (int64_t)n_kv_heads * head_dim)
-        return fail(XATTN_EINVAL, "%s: a row stride is less than the row's heads * head_dim", who);
-    if (q_stride > (int64_t)1 << 32 || k_stride > (int64_t)1 << 32 || v_stride > (int64_t)1 << 32)
-        return fail(XATTN_EUNSUPPORTED, "%s: a row stride exceeds 2^32 values", who);
-    if (q_stride % 8 != 0 || k_stride % 8 != 0 || v_stride % 8 != 0 || misaligned(q, 16) || misaligned(k_new, 16) || misaligned(v_new, 16) ||
-        misaligned(q_out, 16))
-        return fail(XATTN_EINVAL, "%s: q, k_new, v_new, q_out and the row strides must be multiples of 16 bytes", who);
-
-    if (q_out == q && q_stride != (int64_t)n_q_heads * head_dim)
-        return fail(XATTN_EINVAL, "%s: q_out may be q only where q's rows are contiguous", who);
-
-    RopeParams prm = {};
-    prm.q = static_cast<const uint16_t*>(q);
-    prm.k = static_cast<const uint16_t*>(k_new);
-    prm.v = static_cast<const uint16_t*>(v_new);
-    prm.q_stride = q_stride;
-    prm.k_stride = k_stride;
-    prm.v_stride = v_stride;
-    prm.pos = pos;
-    prm.inv_freq = inv_freq;
-    prm.k_ptrs = k_ptrs;
-    prm.v_ptrs = v_ptrs;
-    prm.q_starts = q_starts;
-    prm.kv_lens = kv_lens;
-    prm.q_out = static_cast<uint16_t*>(q_out);
-    prm.batch = batch;
-    prm.total_q = total_q;
-    prm.n_q_heads = n_q_heads;
-    prm.n_kv_heads = n_kv_heads;
-    prm.head_dim = head_dim;
-    prm.frequencies = frequencies;
-    prm.pairs = flags & XATTN_ROPE_PAIRS ? 1 : 0;
-    for (int i = 0, axis = 0; i < frequencies; ++i) {
-        while (left[axis] == 0) axis = (axis + 1) % n_axes;
-        prm.axis_of[i >> 4] |= (uint32_t)axis << (2 * (i & 15));
-        --left[axis];
-        if (flags & XATTN_ROPE_DEALT) axis = (axis + 1) % n_axes;
-    }
     const hipError_t e = launch_rope(prm, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? (int)XATTN_OK : fail_hip(e, "kernel launch");
 }

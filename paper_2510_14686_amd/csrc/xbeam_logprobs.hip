@@ -22,6 +22,7 @@
 #include "../../include/xbeam.h"
 #include "xattn_device.h"
 #include "xattn_launch.h"
+#include "xbeam_logits.h"
 #include "xbeam_logprobs.h"
 
 namespace xattn {
@@ -42,30 +43,6 @@ __device__ __forceinline__ uint32_t order_key(float x) {
 constexpr uint32_t kLowKey = 0x007fffffu;        // of -inf; lesser ones are no value's
 __device__ __forceinline__ float key_value(uint32_t k) { return __uint_as_float(k ^ (k & 0x80000000u ? 0x80000000u : 0xffffffffu)); }
 __device__ __forceinline__ uint64_t candidate(uint32_t key, int index) { return (uint64_t)key << 32 | (uint32_t)~index; }
-
-struct Bf16 {
-    uint16_t bits;
-};
-__device__ __forceinline__ float to_float(Bf16 x) { return __uint_as_float((uint32_t)x.bits << 16); }
-__device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
-__device__ __forceinline__ float to_float(float x) { return x; }
-
-// Sixteen bytes of a row, which may begin anywhere.
-typedef uint32_t words_at_2 __attribute__((ext_vector_type(4), aligned(2)));
-typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
-template <typename T> struct Chunk {
-    static constexpr int kCount = 16 / (int)sizeof(T);
-    u32x4_t x;
-    __device__ __forceinline__ void load(const T* p) {
-        using words = typename std::conditional<sizeof(T) == 4, words_at_4, words_at_2>::type;
-        x = __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
-    }
-    __device__ __forceinline__ float get(int i) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(x[i]);
-        else if constexpr (std::is_same<T, Bf16>::value) return i & 1 ? bf16_hi(x[i >> 1]) : bf16_lo(x[i >> 1]);
-        else return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? x[i >> 1] >> 16 : x[i >> 1]));
-    }
-};
 
 // s and t of some values, and what they are relative to.  While a row is read that is the reference r = m * c as rounded: y = x * c - r is one
 // operation per value, whose terms belong to r itself, so that the sums of lanes and waves meet at the differences of their r, whatever
