@@ -30,14 +30,19 @@ struct MxTile {
     u32x4_t k[4], v[4], vs;
     uint32_t ks;
 };
-__device__ __forceinline__ void load_tile(MxTile& t, const char* kt, const char* vt, int lane) {
-    const int kb = lane >> 4, n = lane & 15;
+// From the tile at kt (vt); `on` false: from nowhere.  The loads go out either way, so that how many are on their way is always known and no wait is
+// for more than it needs.
+__device__ __forceinline__ void load_k(MxTile& t, const char* kt, bool on, int lane) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(kt, on ? kMxTileBytes : 0);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) t.k[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(kt + lane * 16 + 1024 * s));
-    t.ks = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(kt + kMxCodeBytes + lane * 4));
+    for (int s = 0; s < 4; ++s) t.k[s] = load_b128_nt(r, lane * 16, 1024 * s);
+    t.ks = __builtin_amdgcn_raw_buffer_load_b32(r, lane * 4, kMxCodeBytes, 2);
+}
+__device__ __forceinline__ void load_v(MxTile& t, const char* vt, bool on, int lane) {
+    const __amdgpu_buffer_rsrc_t r = make_rsrc(vt, on ? kMxTileBytes : 0);
+    t.vs = load_b128_nt(r, ((lane >> 4) * 4 + ((lane & 15) >> 2)) * 16, kMxCodeBytes);
 #pragma unroll
-    for (int s = 0; s < 4; ++s) t.v[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vt + lane * 16 + 1024 * s));
-    t.vs = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(vt + kMxCodeBytes + (4 * kb + (n >> 2)) * 16));
+    for (int s = 0; s < 4; ++s) t.v[s] = load_b128_nt(r, lane * 16, 1024 * s);
 }
 
 // The scale in byte i of four as a float.
@@ -50,9 +55,9 @@ __device__ __forceinline__ uint32_t unpack(uint32_t codes, float scale) {
 
 // One tile against kTiles times 16 query rows.  s[t][i][j] is the score of key 16 i + 4 kb + j for row n: a lane holds keys of one row, and the
 // products of these with V take them from where they are.
-template <int kTiles>
-__device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], MxTile& r, const bf16x8_t (&qop)[kTiles][4], float scale_log2, int key0, int L,
-                                        const int (&lim)[kTiles], int kb) {
+template <int kTiles, typename NextK, typename NextV>
+__device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], const MxTile& r, const bf16x8_t (&qop)[kTiles][4], float scale_log2, int key0, int L,
+                                        const int (&lim)[kTiles], int kb, NextK next_k, NextV next_v) {
     f32x4_t s[kTiles][4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -67,11 +72,13 @@ __device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], MxTile& r, co
             for (int t = 0; t < kTiles; ++t) s[t][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), qop[t][step], s[t][i], 0, 0, 0);
         }
     }
-    u32x4_t hi[kTiles][2], lo[kTiles][2];
+    next_k();
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) s[t][i] *= scale_log2;
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[t][i][j] *= scale_log2;
         if (__builtin_amdgcn_ballot_w64(key0 + kMxTileTokens > lim[t]) != 0) {      // only tiles that reach a limit
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -97,51 +104,59 @@ __device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], MxTile& r, co
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[t][i][j] = fast_exp2(s[t][i][j] - m_use);
             st[t].l += (s[t][i][0] + s[t][i][1]) + (s[t][i][2] + s[t][i][3]);
-#pragma unroll
-            for (int j = 0; j < 4; j += 2) {
-                const f32x2_t p = {s[t][i][j], s[t][i][j + 1]};
-                const bf16x2_t h = __builtin_convertvector(p, bf16x2_t);
-                const f32x2_t rest = p - __builtin_convertvector(h, f32x2_t);
-                hi[t][i >> 1][(i & 1) * 2 + (j >> 1)] = __builtin_bit_cast(uint32_t, h);
-                lo[t][i >> 1][(i & 1) * 2 + (j >> 1)] = cvt_bf16(rest[0], rest[1]);
-            }
         }
     }
     // What stands behind the sequence's last key may be anything: its weight is 0, and with a scale of 2^-127 so is the product.
+    u32x4_t vs = r.vs;
     if (key0 + kMxTileTokens > L) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        auto known = [&](int i) {
             const int left = L - (key0 + 16 * i + 4 * kb);
-            r.vs[i] &= left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1;
-        }
+            return left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << 8 * left) - 1;
+        };
+        vs = u32x4_t{vs.x & known(0), vs.y & known(1), vs.z & known(2), vs.w & known(3)};
     }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        uint32_t x[8][4];      // token 4 i + r: pairs of values
+        u32x4_t hi[kTiles], lo[kTiles];
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const float scale = scale_of(r.vs[2 * h + i], q);
-                const uint32_t w = r.v[2 * h + i][q];
-                x[4 * i + q][0] = unpack<0>(w, scale);
-                x[4 * i + q][1] = unpack<1>(w, scale);
-                x[4 * i + q][2] = unpack<2>(w, scale);
-                x[4 * i + q][3] = unpack<3>(w, scale);
+            for (int i = 0; i < 4; ++i) {
+                const f32x2_t p = {s[t][2 * h + (i >> 1)][2 * (i & 1)], s[t][2 * h + (i >> 1)][2 * (i & 1) + 1]};
+                const bf16x2_t b = __builtin_convertvector(p, bf16x2_t);
+                const f32x2_t rest = p - __builtin_convertvector(b, f32x2_t);
+                hi[t][i] = __builtin_bit_cast(uint32_t, b);
+                lo[t][i] = cvt_bf16(rest[0], rest[1]);
             }
+        float scale[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;      // high or low halves of both words
-            u32x4_t a;
+        for (int i = 0; i < 8; ++i) scale[i] = scale_of(vs[2 * h + (i >> 2)], i & 3);
+        // A byte of the codes at a time, of eight tokens: two of the lane's eight values.
+        auto two = [&](auto byte) {
+            constexpr int kByte = decltype(byte)::value;
+            uint32_t x[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(x[2 * i + 1][e >> 1], x[2 * i][e >> 1], sel);
+            for (int i = 0; i < 8; ++i) x[i] = unpack<kByte>(r.v[2 * h + (i >> 2)][i & 3], scale[i]);
 #pragma unroll
-            for (int t = 0; t < kTiles; ++t) {
-                st[t].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, hi[t][h]), st[t].o[e], 0, 0, 0);
-                st[t].o[e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, lo[t][h]), st[t].o[e], 0, 0, 0);
+            for (int half = 0; half < 2; ++half) {
+                u32x4_t a;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], half ? 0x07060302u : 0x05040100u);
+#pragma unroll
+                for (int t = 0; t < kTiles; ++t) {
+                    f32x4_t& o = st[t].o[2 * kByte + half];
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, hi[t]), o, 0, 0, 0);
+                    o = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, lo[t]), o, 0, 0, 0);
+                }
             }
-        }
+        };
+        two(std::integral_constant<int, 0>());
+        two(std::integral_constant<int, 1>());
+        two(std::integral_constant<int, 2>());
+        two(std::integral_constant<int, 3>());
+        __builtin_amdgcn_sched_barrier(0);
     }
+    next_v();
 }
 
 // A segment in flight: its Q operand, its limits and its first tile.  seg.j0 and j1 are positions of the stream, seg.L tokens.
@@ -161,7 +176,8 @@ __device__ __forceinline__ void mx_begin(MxCtx<kTiles>& c, const DecodeParams& p
     const int64_t at = ((int64_t)(seg.j0 / kMxPositions) * prm.n_kv_heads + seg.kvh) * kMxTileBytes;
     c.kp = static_cast<const char*>(seg.kp) + at;
     c.vp = static_cast<const char*>(seg.vp) + at;
-    load_tile(c.first, c.kp, c.vp, lane);
+    load_k(c.first, c.kp, true, lane);
+    load_v(c.first, c.vp, true, lane);
     // Q through a descriptor over the sequence's rows: rows past n_rows lie past its end and read as zero.
     const int seq_rows = prm.q_len * prm.n_q_heads;
     const __amdgpu_buffer_rsrc_t rq = make_rsrc(prm.q + (long)seg.b * seq_rows * kHeadDim, (uint32_t)(seq_rows * kRowBytes));
@@ -189,15 +205,22 @@ __device__ __forceinline__ void mx_run(MatrixState (&st)[kTiles], MxCtx<kTiles>&
     }
     const int64_t step = (int64_t)prm.n_kv_heads * kMxTileBytes;
     const int first = c.seg.j0 / kMxPositions, n_tiles = c.seg.j1 / kMxPositions - first;
+    // Two tiles in registers, and where one's codes have been used the loads of the tile after the next go out into their place.
+    auto k_at = [&](int i) { return c.kp + i * step; };
+    auto v_at = [&](int i) { return c.vp + i * step; };
     MxTile other;
-    int i = 0;
-    for (; i + 2 <= n_tiles; i += 2) {
-        load_tile(other, c.kp + (i + 1) * step, c.vp + (i + 1) * step, lane);
-        mx_tile<kTiles>(st, c.first, c.qop, prm.scale_log2, (first + i) * kMxTileTokens, c.seg.L, c.lim, kb);
-        if (i + 2 < n_tiles) load_tile(c.first, c.kp + (i + 2) * step, c.vp + (i + 2) * step, lane);
-        mx_tile<kTiles>(st, other, c.qop, prm.scale_log2, (first + i + 1) * kMxTileTokens, c.seg.L, c.lim, kb);
+    load_k(other, k_at(1), n_tiles > 1, lane);
+    load_v(other, v_at(1), n_tiles > 1, lane);
+    auto tile = [&](int i, MxTile& r) {
+        const bool more = i + 2 < n_tiles;
+        mx_tile<kTiles>(st, r, c.qop, prm.scale_log2, (first + i) * kMxTileTokens, c.seg.L, c.lim, kb,
+                        [&] { load_k(r, k_at(i + 2), more, lane); __builtin_amdgcn_sched_barrier(0); }, [&] { load_v(r, v_at(i + 2), more, lane); });
+    };
+    for (int i = 0; i < n_tiles; i += 2) {
+        tile(i, c.first);
+        if (i + 1 >= n_tiles) break;
+        tile(i + 1, other);
     }
-    if (i < n_tiles) mx_tile<kTiles>(st, c.first, c.qop, prm.scale_log2, (first + i) * kMxTileTokens, c.seg.L, c.lim, kb);
 }
 
 // grid.x = workgroups of pieces times groups of R query rows, grid.z = KV heads.  (What the plan needs are arguments of their own: see
