@@ -32,12 +32,34 @@ constexpr int kMxNanScale = 255;
 
 // Positions of the token stream (see xattn_plan.h) that a tile takes, whose rounding of piece bounds then is to whole tiles.
 constexpr int kMxPositions = kPlanRound;
-constexpr int kMxWaves = 8;                  // waves of a workgroup, which share a piece
 XATTN_HD int mx_positions(int len) { return len > 0 ? (int)(((unsigned)len + (kMxTileTokens - 1)) / kMxTileTokens) * kMxPositions : 0; }
+// Positions of each of `parts` waves of a piece of `len` positions, all but the last one's: whole tiles.
+XATTN_HD int mx_part_positions(int len, int parts) { return ((len + parts - 1) / parts + kMxPositions - 1) / kMxPositions * kMxPositions; }
 
-// Decode attention; prm.share is not used.
-hipError_t launch_decode_mx(const DecodeParams& prm, hipStream_t stream);
-int mx_rows_per_wave(int rows_total);
+// How a call's work is cut: `waves` waves of a workgroup share a piece, of which there are `pieces`.
+struct MxCut {
+    int rows, waves, pieces;
+};
+constexpr int kMxComputeUnits = 256;
+// A compute unit holds twelve waves with 16 query rows each, or eight with 32 (registers and LDS).  One workgroup of all of them leaves the fewest
+// partial results, and where that many workgroups fill the chip (8 KV heads: 32 pieces) is faster than several small ones: 128 sequences of 1028 to
+// 8196 tokens, 16 rows of 8 KV heads 107.4 us, 116.3 in workgroups of four.  Pieces come in multiples of eight, though, and with many KV heads, or a number of them that
+// does not go into 256, a quarter of the chip or more may have nothing to do in the last round: small ones then, 16 sequences of 501 to
+// 4001 tokens of 40 KV heads 48.4 -> 37.5.
+inline MxCut mx_cut(int q_len, int n_q_heads, int n_kv_heads) {
+    const int rows_total = n_q_heads / n_kv_heads * q_len, rows = rows_total <= 16 ? 16 : 32;
+    const int most = rows == 16 ? 12 : 8, on_a_piece = (rows_total + rows - 1) / rows * n_kv_heads;
+    auto used = [&](int at_once, int pieces) {      // per mille of the rounds' places
+        const int n = pieces * on_a_piece;
+        return (int)(1000L * n / ((n + at_once - 1) / at_once * at_once));
+    };
+    const int small = kMxComputeUnits * most / 4, pieces = pieces_of(kMxComputeUnits, on_a_piece), more = pieces_of(small, on_a_piece);
+    if (used(kMxComputeUnits, pieces) < 800 && used(small, more) > used(kMxComputeUnits, pieces)) return MxCut{rows, 4, more};
+    return MxCut{rows, most, pieces};
+}
+
+// Decode attention; prm.share and parts are not used.
+hipError_t launch_decode_mx(const DecodeParams& prm, const MxCut& cut, hipStream_t stream);
 
 // Rotation and append: prm.k_ptrs and v_ptrs are ranges of tiles, prm.head_dim is 128.
 hipError_t launch_rope_mx(const RopeParams& prm, hipStream_t stream);

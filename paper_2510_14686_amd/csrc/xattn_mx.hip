@@ -22,6 +22,8 @@ struct TileUnit {
     static __device__ __forceinline__ int stream(int raw, int seg_cost) { return raw > 0 ? mx_positions(raw) + seg_cost : 0; }
 };
 
+constexpr float kSlack = 8.0f;
+
 // Fixed work of a (piece, sequence) segment, in positions.
 constexpr int kMxSegCost = kMxPositions;
 
@@ -45,8 +47,9 @@ __device__ __forceinline__ void load_v(MxTile& t, const char* vt, bool on, int l
     for (int s = 0; s < 4; ++s) t.v[s] = load_b128_nt(r, lane * 16, 1024 * s);
 }
 
-// The scale in byte i of four as a float.
-__device__ __forceinline__ float scale_of(uint32_t bytes, int i) { return __uint_as_float((i == 3 ? bytes >> 1 : bytes << (23 - 8 * i)) & 0x7f800000u); }
+// The scale in byte i of four as a float's exponent.  The conversion takes no more of a scale than that; what stands in the other bits does not matter
+// (masking them off: 24 instructions of a tile's 430).
+__device__ __forceinline__ float scale_of(uint32_t bytes, int i) { return __uint_as_float(i == 3 ? bytes >> 1 : bytes << (23 - 8 * i)); }
 // The codes in byte i of four, times the scale, as two bf16: exact.
 template <int kByte>
 __device__ __forceinline__ uint32_t unpack(uint32_t codes, float scale) {
@@ -75,10 +78,6 @@ __device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], const MxTile&
     next_k();
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) s[t][i][j] *= scale_log2;
         if (__builtin_amdgcn_ballot_w64(key0 + kMxTileTokens > lim[t]) != 0) {      // only tiles that reach a limit
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -88,12 +87,12 @@ __device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], const MxTile&
         float mx = kNegInf;
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(fmaxf(s[t][i][0], s[t][i][1]), fmaxf(s[t][i][2], s[t][i][3])));
-        mx = kb_max(mx);
-        const bool moves = mx > st[t].m;
-        if (__builtin_amdgcn_ballot_w64(moves) != 0) {
-            const float m_new = moves ? mx : st[t].m;
-            const float alpha = moves ? fast_exp2(st[t].m - m_new) : 1.0f;
-            st[t].m = m_new;
+        // The reference moves when a score exceeds it by 2^8 or more: no weight exceeds that, and few tiles move it.
+        if (__builtin_amdgcn_ballot_w64(mx * scale_log2 > st[t].m + kSlack) != 0) {
+            mx = kb_max(mx) * scale_log2;
+            const bool moves = mx > st[t].m;
+            const float alpha = moves ? fast_exp2(st[t].m - mx) : 1.0f;
+            st[t].m = moves ? mx : st[t].m;
             st[t].l *= alpha;
 #pragma unroll
             for (int e = 0; e < 8; ++e) st[t].o[e] *= alpha;
@@ -102,7 +101,7 @@ __device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], const MxTile&
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) s[t][i][j] = fast_exp2(s[t][i][j] - m_use);
+            for (int j = 0; j < 4; ++j) s[t][i][j] = fast_exp2(__builtin_fmaf(s[t][i][j], scale_log2, -m_use));
             st[t].l += (s[t][i][0] + s[t][i][1]) + (s[t][i][2] + s[t][i][3]);
         }
     }
@@ -178,6 +177,8 @@ __device__ __forceinline__ void mx_begin(MxCtx<kTiles>& c, const DecodeParams& p
     c.vp = static_cast<const char*>(seg.vp) + at;
     load_k(c.first, c.kp, true, lane);
     load_v(c.first, c.vp, true, lane);
+    // The kernel takes a positive scale: a negative one's sign and a zero go into Q.
+    const uint32_t q_and = prm.scale_log2 == 0.0f ? 0u : 0xffffffffu, q_xor = prm.scale_log2 < 0.0f ? 0x80008000u : 0u;
     // Q through a descriptor over the sequence's rows: rows past n_rows lie past its end and read as zero.
     const int seq_rows = prm.q_len * prm.n_q_heads;
     const __amdgpu_buffer_rsrc_t rq = make_rsrc(prm.q + (long)seg.b * seq_rows * kHeadDim, (uint32_t)(seq_rows * kRowBytes));
@@ -188,7 +189,7 @@ __device__ __forceinline__ void mx_begin(MxCtx<kTiles>& c, const DecodeParams& p
         const int qoff = (row_ok ? seq_row(prm, seg, r) : seq_rows) * kRowBytes + kb * 64;
 #pragma unroll
         for (int step = 0; step < 4; ++step)
-            c.qop[t][step] = __builtin_bit_cast(bf16x8_t, __builtin_amdgcn_raw_buffer_load_b128(rq, qoff + 16 * step, 0, 0));
+            c.qop[t][step] = __builtin_bit_cast(bf16x8_t, (__builtin_amdgcn_raw_buffer_load_b128(rq, qoff + 16 * step, 0, 0) & q_and) ^ q_xor);
         c.lim[t] = seg.L - prm.q_len + row_token(prm, seg.row0 + r) + 1;
     }
 }
@@ -206,44 +207,38 @@ __device__ __forceinline__ void mx_run(MatrixState (&st)[kTiles], MxCtx<kTiles>&
     const int64_t step = (int64_t)prm.n_kv_heads * kMxTileBytes;
     const int first = c.seg.j0 / kMxPositions, n_tiles = c.seg.j1 / kMxPositions - first;
     // Two tiles in registers, and where one's codes have been used the loads of the tile after the next go out into their place.
+    const float scale_log2 = prm.scale_log2 == 0.0f ? 1.0f : fabsf(prm.scale_log2);
     auto k_at = [&](int i) { return c.kp + i * step; };
     auto v_at = [&](int i) { return c.vp + i * step; };
-    MxTile other;
-    load_k(other, k_at(1), n_tiles > 1, lane);
-    load_v(other, v_at(1), n_tiles > 1, lane);
     auto tile = [&](int i, MxTile& r) {
-        const bool more = i + 2 < n_tiles;
-        mx_tile<kTiles>(st, r, c.qop, prm.scale_log2, (first + i) * kMxTileTokens, c.seg.L, c.lim, kb,
-                        [&] { load_k(r, k_at(i + 2), more, lane); __builtin_amdgcn_sched_barrier(0); }, [&] { load_v(r, v_at(i + 2), more, lane); });
+        const bool more = i + 1 < n_tiles;
+        mx_tile<kTiles>(st, r, c.qop, scale_log2, (first + i) * kMxTileTokens, c.seg.L, c.lim, kb,
+                        [&] { load_k(r, k_at(i + 1), more, lane); __builtin_amdgcn_sched_barrier(0); }, [&] { load_v(r, v_at(i + 1), more, lane); });
     };
-    for (int i = 0; i < n_tiles; i += 2) {
-        tile(i, c.first);
-        if (i + 1 >= n_tiles) break;
-        tile(i + 1, other);
-    }
+    for (int i = 0; i < n_tiles; ++i) tile(i, c.first);
 }
 
 // grid.x = workgroups of pieces times groups of R query rows, grid.z = KV heads.  (What the plan needs are arguments of their own: see
 // split_decode_kernel, whose walk over a piece this one shares.)
-template <int R>
-__global__ __launch_bounds__(64 * kMxWaves) void decode_mx_kernel(const int32_t* __restrict__ kv_lens, const void* const* k_ptrs, const void* const* v_ptrs,
+template <int R, int kWaves>
+__global__ __launch_bounds__(64 * kWaves, R == 16 ? 3 : 2) void decode_mx_kernel(const int32_t* __restrict__ kv_lens, const void* const* k_ptrs, const void* const* v_ptrs,
                                                                  int batch, int n_pieces, int min_piece, int few_pieces, int few_min,
                                                                  int xcd_skew, int grid_x, DecodeParams prm) {
     constexpr int kTiles = R / 16;
-    constexpr int kStates = (kMxWaves - 1) * kTiles;
-    __shared__ __attribute__((aligned(16))) char lds[kMxWaves * kLdsPerWave + kStates * kLdsPerState];
+    constexpr int kStates = (kWaves - 1) * kTiles;
+    __shared__ __attribute__((aligned(16))) char lds[kWaves * kLdsPerWave + kStates * kLdsPerState];
     const int lane = threadIdx.x & 63;
     const int part = uniform((int)(threadIdx.x >> 6));
     SeqWindow win;
     const WavePlan wp = wave_plan<TileUnit>(kv_lens, k_ptrs, v_ptrs, batch, n_pieces, min_piece, kMxSegCost, xcd_skew, FewPieces{few_pieces, few_min}, lane,
-                                            &win, kMxWaves);
+                                            &win, kWaves);
     const Plan& pl = wp.pl;
     const int bid = blockIdx.x, rows_total = prm.group * prm.q_len;
     const DecodeWork work = decode_work(pl, grid_x, 1, rows_total, R, bid, 0);
     const int p = work.piece, rows = work.rows;
     const int piece0 = piece_bound(pl, p), piece1 = piece_bound(pl, p + 1);
-    const int sub = part_positions(piece1 - piece0, kMxWaves), s0 = piece0 + part * sub, s1 = s0 + sub < piece1 ? s0 + sub : piece1;
-    if (__builtin_expect(64 * (grid_x - 1 - bid) < batch && blockIdx.z == 0 && part == kMxWaves - 1, 0)) {
+    const int sub = mx_part_positions(piece1 - piece0, kWaves), s0 = piece0 + part * sub, s1 = s0 + sub < piece1 ? s0 + sub : piece1;
+    if (__builtin_expect(64 * (grid_x - 1 - bid) < batch && blockIdx.z == 0 && part == kWaves - 1, 0)) {
         for (int g = grid_x - 1 - bid; 64 * g < batch; g += grid_x)
             wave_write_meta<TileUnit>(wp, kv_lens, batch, prm.q_len * prm.n_q_heads, g, lane, prm.meta);
     }
@@ -283,7 +278,7 @@ __global__ __launch_bounds__(64 * kMxWaves) void decode_mx_kernel(const int32_t*
     char* const lds_wave = lds + part * kLdsPerWave;
     auto run_piece = [&](auto tiles) {
         constexpr int kT = decltype(tiles)::value;
-        auto state_of = [&](int of_part, int t) { return lds + kMxWaves * kLdsPerWave + ((of_part - 1) * kT + t) * kLdsPerState; };
+        auto state_of = [&](int of_part, int t) { return lds + kWaves * kLdsPerWave + ((of_part - 1) * kT + t) * kLdsPerState; };
         MatrixState st[kT];
         MxCtx<kT> cur;
         int positions = 0;
@@ -332,19 +327,19 @@ __global__ __launch_bounds__(64 * kMxWaves) void decode_mx_kernel(const int32_t*
     else run_piece(std::integral_constant<int, kTiles>());
 }
 
-template <int R>
-hipError_t launch_r(const DecodeParams& prm, hipStream_t stream) {
+template <int R, int kWaves>
+hipError_t launch_with(const DecodeParams& prm, hipStream_t stream) {
     const int grid_x = decode_grid_x(prm.n_pieces, 1, prm.group * prm.q_len, R);
-    return launch(decode_mx_kernel<R>, dim3((unsigned)grid_x, 1, (unsigned)prm.n_kv_heads), 64 * kMxWaves, stream, prm.kv_lens, prm.k_ptrs, prm.v_ptrs, prm.batch,
-                  prm.n_pieces, prm.min_piece_tokens, prm.few.pieces, prm.few.min_piece, prm.xcd_skew, grid_x, prm);
+    return launch(decode_mx_kernel<R, kWaves>, dim3((unsigned)grid_x, 1, (unsigned)prm.n_kv_heads), 64 * kWaves, stream, prm.kv_lens, prm.k_ptrs, prm.v_ptrs,
+                  prm.batch, prm.n_pieces, prm.min_piece_tokens, prm.few.pieces, prm.few.min_piece, prm.xcd_skew, grid_x, prm);
 }
 
 }  // namespace
 
-int mx_rows_per_wave(int rows_total) { return rows_total <= 16 ? 16 : 32; }
-
-hipError_t launch_decode_mx(const DecodeParams& prm, hipStream_t stream) {
-    const hipError_t e = mx_rows_per_wave(prm.group * prm.q_len) == 16 ? launch_r<16>(prm, stream) : launch_r<32>(prm, stream);
+hipError_t launch_decode_mx(const DecodeParams& prm, const MxCut& cut, hipStream_t stream) {
+    hipError_t e;
+    if (cut.rows == 16) e = cut.waves == 12 ? launch_with<16, 12>(prm, stream) : launch_with<16, 4>(prm, stream);
+    else e = cut.waves == 8 ? launch_with<32, 8>(prm, stream) : launch_with<32, 4>(prm, stream);
     return e != hipSuccess ? e : launch_decode_merge(prm, stream);
 }
 

@@ -14,16 +14,9 @@ namespace xattn {
 
 namespace {
 
-constexpr int kComputeUnits = 256;
 constexpr int kMaxVerifyBatch = 4096, kMaxVerifyQLen = 16, kMaxVerifyVocab = 1 << 24;
 
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
-
-// Pieces of a decode call: a workgroup per compute unit works on one of them for a KV head and a group of query rows.
-int mx_pieces(int q_len, int n_q_heads, int n_kv_heads) {
-    const int rows_total = n_q_heads / n_kv_heads * q_len, rows = mx_rows_per_wave(rows_total);
-    return pieces_of(kComputeUnits, (rows_total + rows - 1) / rows * n_kv_heads);
-}
 
 int check_verify(const char* who, int batch, int q_len, int vocab) {
     if (batch < 1 || q_len < 1 || vocab < 1) return fail(XATTN_EINVAL, "%s: batch, q_len and vocab must be positive", who);
@@ -62,7 +55,7 @@ size_t xattn_mx_range_bytes(int64_t tokens, int n_kv_heads, int head_dim) {
 
 size_t xattn_decode_mx_workspace_bytes(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim) {
     if (check_decode_shape(batch, q_len, n_q_heads, n_kv_heads, head_dim) != XATTN_OK) return 0;
-    return decode_layout(batch, q_len, n_q_heads, mx_pieces(q_len, n_q_heads, n_kv_heads)).total;
+    return decode_layout(batch, q_len, n_q_heads, mx_cut(q_len, n_q_heads, n_kv_heads).pieces).total;
 }
 
 int xattn_decode_mx(const void* q, const void* const* k_ptrs, const void* const* v_ptrs, const int32_t* kv_lens, int batch, int q_len,
@@ -90,21 +83,23 @@ int xattn_decode_mx(const void* q, const void* const* k_ptrs, const void* const*
     prm.scale_log2 = scale_log2;
     prm.out = static_cast<uint16_t*>(out);
     prm.lse = lse;
-    prm.n_pieces = mx_pieces(q_len, n_q_heads, n_kv_heads);
-    prm.min_piece_tokens = kMxWaves * kMxPositions;
+    const MxCut cut = mx_cut(q_len, n_q_heads, n_kv_heads);
+    prm.n_pieces = cut.pieces;
+    prm.min_piece_tokens = cut.waves * kMxPositions;
     prm.few = FewPieces{prm.n_pieces, kMxPositions};
     prm.xcd_skew = 0;
     struct Call {
         DecodeParams* prm;
+        const MxCut* cut;
         DecodeLayout w;
         hipStream_t stream;
-    } call = {&prm, decode_layout(batch, q_len, n_q_heads, prm.n_pieces), static_cast<hipStream_t>(stream)};
+    } call = {&prm, &cut, decode_layout(batch, q_len, n_q_heads, cut.pieces), static_cast<hipStream_t>(stream)};
     return with_workspace(who, call.w.total, stream, [](void* context, char* ws) {
         const Call& c = *static_cast<Call*>(context);
         c.prm->meta = reinterpret_cast<int32_t*>(ws + c.w.meta_off);
         c.prm->part_ml = reinterpret_cast<float*>(ws + c.w.ml_off);
         c.prm->part_o = reinterpret_cast<float*>(ws + c.w.o_off);
-        const hipError_t e = launch_decode_mx(*c.prm, c.stream);
+        const hipError_t e = launch_decode_mx(*c.prm, *c.cut, c.stream);
         return e == hipSuccess ? (int)XATTN_OK : fail_hip(e, "kernel launch");
     }, &call);
 }
