@@ -44,7 +44,7 @@ inline VerifyCut verify_cut(long rows, int vocab, int workgroups) {
     const int size = (int)((steps + parts - 1) / parts) * kVerifyStep;
     return VerifyCut{(vocab + size - 1) / size, size};
 }
-constexpr int kVerifyReaders = 2048, kVerifyPickers = 1024;      // workgroups of the two passes
+constexpr int kVerifyReaders = 8192, kVerifyPickers = 4096;      // workgroups of the two passes
 struct VerifyLayout {
     VerifyCut read, pick;
     size_t best_off, sums_off, decisions_off, total;

@@ -4,10 +4,11 @@
 //   At the first t that falls, the new token comes from w = max(0, p_t - q_t), without one that falls from w = p behind the last draft:
 //   the least i with sum_{j <= i} w_j > u W.  E[emitted] is p's whatever q is.
 //
-// Three passes (four with a draft's probabilities):
-//   read     every row once, in parts: a reference and the sum of exponentials, in 32 bits; what a draft's fate is decided by
-//   weigh    which drafts stand, and the sums of p and q of the row that the new token comes from, part by part, in 64 bits
-//   rest     the sums of max(0, p - q), part by part
+// Steps, a kernel each:
+//   read     every row once, in parts: a reference and the sum of exponentials, in 32 bits
+//   decide   which drafts stand; the end of it with XBEAM_GREEDY
+//   weigh    the sums of p and q of the row that the new token comes from, part by part, in 64 bits
+//   rest     the sums of max(0, p - q), part by part (with a draft's probabilities only)
 //   pick     the part that the random number falls into, and the token in it
 // 64 bits because the borders between 100000 tokens lie 10^-5 apart on average and closer where it matters: with sums in 32 bits one token in
 // a hundred would be another one's neighbour.  The row's probabilities are worked out anew in every pass: to keep them would be 8 bytes per logit.
@@ -56,35 +57,52 @@ __device__ __forceinline__ void load_logits(const T* p, int left, float (&x)[8])
     }
 }
 
-__device__ __forceinline__ double wave_sum_d(double x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d, 64);
-    return x;
+template <int kCtrl, int kRows>
+__device__ __forceinline__ double dpp_add_d(double x) {
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, kCtrl, kRows, 0xf, true);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)(u >> 32), kCtrl, kRows, 0xf, true);
+    return x + __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
 }
-__device__ __forceinline__ double wave_max_d(double x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x = fmax(x, __shfl_xor(x, d, 64));
-    return x;
+// Inclusive sums over the lanes, as wave_incl_scan_i makes them.
+__device__ __forceinline__ double wave_scan_d(double x) {
+    x = dpp_add_d<0x111, 0xf>(x);
+    x = dpp_add_d<0x112, 0xf>(x);
+    x = dpp_add_d<0x114, 0xf>(x);
+    x = dpp_add_d<0x118, 0xf>(x);
+    x = dpp_add_d<0x142, 0xa>(x);
+    return dpp_add_d<0x143, 0xc>(x);
 }
+__device__ __forceinline__ double lane_d(double x, int lane) {      // lane: wave-uniform
+    const uint64_t u = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)u, lane), hi = (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(u >> 32), lane);
+    return __builtin_bit_cast(double, (uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum_d(double x) { return lane_d(wave_scan_d(x), 63); }
 
-// 2^y for y <= 0, to 2^-51 of it: 2^n by the exponent, 2^f for |f| <= 1/2 by twelve terms of its series.
+// 2^y, to 2^-45 of it: 2^n by the exponent, 2^f for |f| <= 1/2 by the polynomial that meets it at the ten Chebyshev nodes there.  0 from -2000 on
+// down and for NaN.
 __device__ __forceinline__ double exp2_d(double y) {
-    y = fmax(y, -1100.0);
+    y = fmax(y, -2000.0);
     const double n = rint(y), f = y - n;
-    double p = 2.5678435993488202e-11;                         // (ln 2)^k / k!
-    p = __builtin_fma(p, f, 4.4455382718708116e-10);
-    p = __builtin_fma(p, f, 7.0549116208011233e-09);
-    p = __builtin_fma(p, f, 1.0178086009239699e-07);
-    p = __builtin_fma(p, f, 1.3215486790144309e-06);
-    p = __builtin_fma(p, f, 1.5252733804059841e-05);
-    p = __builtin_fma(p, f, 1.5403530393381609e-04);
-    p = __builtin_fma(p, f, 1.3333558146428443e-03);
-    p = __builtin_fma(p, f, 9.6181291076284772e-03);
-    p = __builtin_fma(p, f, 5.5504108664821580e-02);
-    p = __builtin_fma(p, f, 2.4022650695910072e-01);
-    p = __builtin_fma(p, f, 6.9314718055994531e-01);
-    p = __builtin_fma(p, f, 1.0);
+    double p = 1.0205905413765595e-07;
+    p = __builtin_fma(p, f, 1.325964524488711e-06);
+    p = __builtin_fma(p, f, 1.5252672924850737e-05);
+    p = __builtin_fma(p, f, 1.540343375125101e-04);
+    p = __builtin_fma(p, f, 1.3333558200794592e-03);
+    p = __builtin_fma(p, f, 9.618129193934313e-03);
+    p = __builtin_fma(p, f, 5.550410866465167e-02);
+    p = __builtin_fma(p, f, 2.402265069564034e-01);
+    p = __builtin_fma(p, f, 6.931471805599462e-01);
+    p = __builtin_fma(p, f, 1.0000000000000135);
     return ldexp(p, (int)n);
+}
+// log2 of a positive number, to 2^-43: the instruction's 32 bits, and what is left of x over 2^that, 1 + r with |r| < 2^-20.
+__device__ __forceinline__ double log2_d(double x) {
+    const int e = __builtin_amdgcn_frexp_exp(x);
+    const double y = __builtin_amdgcn_frexp_mant(x), l = (double)__builtin_amdgcn_logf((float)y);
+    const double r = __builtin_fma(y, exp2_d(-l), -1.0);
+    return x > 0.0 && x < __builtin_inf() ? (double)e + l + (r - 0.5 * r * r) * kLog2e : x == 0.0 ? -__builtin_inf() : __builtin_nan("");
 }
 
 // Order of logits as whole numbers: value, then the lowest index; NaN below everything.
@@ -93,6 +111,9 @@ __device__ __forceinline__ uint64_t token_key(float x, int index) {
     return (uint64_t)(x == x ? k : 0u) << 32 | (uint32_t)~index;
 }
 
+// What a logit's exponent is, in log2 units: the same rounded factor wherever the first pass' sums are used.
+__device__ __forceinline__ float exponent_scale(float scale) { return (float)((double)scale * kLog2e); }
+
 __device__ __forceinline__ int drafts_of(const VerifyParams& prm, int b) {
     const int n = prm.n_drafts ? prm.n_drafts[b] : prm.q_len - 1;
     return n < 0 ? 0 : n < prm.q_len ? n : prm.q_len - 1;
@@ -100,7 +121,7 @@ __device__ __forceinline__ int drafts_of(const VerifyParams& prm, int b) {
 
 // ---------------------------------------------------------------------------------- read
 // grid.x = rows, those of the target, then those of the draft; grid.y = parts.
-template <typename T>
+template <typename T, bool kGreedy>
 __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParams prm, VerifyCut cut) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = blockIdx.y;
     const int target_rows = prm.batch * prm.q_len, row = blockIdx.x;
@@ -109,16 +130,21 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
     const int b = r / per, t = r - b * per, n = drafts_of(prm, b);
     if (t >= n + (is_draft ? 0 : 1)) return;      // a row that no token is drawn from or judged by
     const T* const p = static_cast<const T*>(is_draft ? prm.draft : prm.target) + (int64_t)r * (is_draft ? prm.draft_stride : prm.target_stride);
-    const float c = (float)((double)(is_draft ? prm.draft_scale : prm.scale) * kLog2e);
+    const float c = exponent_scale(is_draft ? prm.draft_scale : prm.scale);
     const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
     float m = kNegInf, ref = 0.0f, sum = 0.0f;
     uint64_t best = 0;
-    for (int i = first + 8 * tid; i < end; i += kVerifyStep) {
-        float x[8];
-        load_logits(p + i, end - i, x);
-        float top = x[0];
+    // Four steps' loads go out together, and the running reference is looked at once for them.
+    auto steps = [&](auto count, int i) {
+        constexpr int kCount = decltype(count)::value;
+        float x[kCount][8];
 #pragma unroll
-        for (int j = 1; j < 8; ++j) top = fmaxf(top, x[j]);
+        for (int k = 0; k < kCount; ++k) load_logits(p + i + k * kVerifyStep, end - i - k * kVerifyStep, x[k]);
+        float top = x[0][0];
+#pragma unroll
+        for (int k = 0; k < kCount; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, x[k][j]);
         if (top > m) {
             const float to = top * c;
             sum *= fast_exp2(m == kNegInf ? 0.0f : ref - to);
@@ -126,30 +152,36 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
             ref = to;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            sum += fast_exp2(__builtin_fmaf(x[j], c, -ref));
-            if (prm.greedy) {
-                const uint64_t key = i + j < end ? token_key(x[j], i + j) : 0;
-                best = key > best ? key : best;
+        for (int k = 0; k < kCount; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sum += fast_exp2(__builtin_fmaf(x[k][j], c, -ref));
+                if constexpr (kGreedy) {
+                    const int at = i + k * kVerifyStep + j;
+                    const uint64_t key = at < end ? token_key(x[k][j], at) : 0;
+                    best = key > best ? key : best;
+                }
             }
-        }
-    }
+    };
+    int i = first + 8 * tid;
+    for (; i + 3 * kVerifyStep < end; i += 4 * kVerifyStep) steps(std::integral_constant<int, 4>(), i);
+    for (; i < end; i += kVerifyStep) steps(std::integral_constant<int, 1>(), i);
     __shared__ float refs[kWaves], sums[kWaves];
     __shared__ uint64_t keys[kWaves];
     const float mine = m == kNegInf ? kNegInf : ref, top = wave_max(mine);
     // a lane of nothing but -inf has 0, one with a NaN NaN
     const float s = wave_sum(sum * (mine == kNegInf ? (sum == sum ? 0.0f : sum) : fast_exp2(mine - top)));
-    if (prm.greedy) {
+    if constexpr (kGreedy) {
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
             const uint64_t other = __shfl_xor(best, d, 64);
             best = other > best ? other : best;
         }
+        if (lane == 0) keys[wave] = best;
     }
     if (lane == 0) {
         refs[wave] = top;
         sums[wave] = s;
-        keys[wave] = best;
     }
     __syncthreads();
     if (tid > 0) return;
@@ -158,38 +190,53 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
     float total = 0.0f;
     for (int w = 0; w < kWaves; ++w) {
         total += refs[w] == kNegInf ? sums[w] : sums[w] * fast_exp2(refs[w] - all);
-        best = keys[w] > best ? keys[w] : best;
+        if constexpr (kGreedy) best = keys[w] > best ? keys[w] : best;
     }
     prm.stats[(int64_t)row * cut.parts + part] = make_float2(all, total);
-    if (prm.greedy) prm.best[(int64_t)row * cut.parts + part] = best;
+    if constexpr (kGreedy) prm.best[(int64_t)row * cut.parts + part] = best;
 }
 
-// ---------------------------------------------------------------------------------- weigh
-// log2 of a row's sum of exponentials, and the largest exponent; NaN where the row has no probabilities.  By one wave.
+// ---------------------------------------------------------------------------------- decide
+// A row's largest exponent (as the first pass rounded it) and log2 of its sum; NaN where it has no probabilities.  By one wave.
 struct RowSum {
     double log2_sum, top;
 };
-__device__ __forceinline__ RowSum row_sum(const float2* stats, int parts, int lane) {
-    const float2 mine = lane < parts ? stats[lane] : make_float2(kNegInf, 0.0f);
-    const double top = wave_max_d((double)mine.x);
-    const double s = wave_sum_d(mine.x == kNegInf ? (double)mine.y : (double)mine.y * exp2((double)mine.x - top));
-    return RowSum{log2(s) + top, top};
+__device__ __forceinline__ RowSum row_sum(float2 mine) {
+    const float top = wave_max(mine.x);
+    const double s = wave_sum_d(mine.x == kNegInf ? (double)mine.y : (double)mine.y * exp2_d((double)mine.x - (double)top));
+    return RowSum{log2_d(s) + (double)top, (double)top};
 }
 template <typename T>
 __device__ __forceinline__ double logit_at(const void* rows, int64_t stride, int64_t row, int token) { return (double)to_float(static_cast<const T*>(rows)[row * stride + token]); }
 
-// Sequence b's drafts, by all waves; the outputs that are known.
-template <typename T>
-__device__ __forceinline__ Decision decide(const VerifyParams& prm, const VerifyCut& cut, int b, int tid, bool writes) {
+// A workgroup per sequence, a wave per row: which drafts stand, and the outputs that are known with that.
+constexpr int kDecideWaves = 8;
+template <typename T, bool kGreedy>
+__global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(VerifyParams prm, VerifyCut cut) {
     __shared__ double lses[16], tops[16], draft_tops[16], lps[16];
     __shared__ int stands[16], tokens[16];
-    const int lane = tid & 63, wave = tid >> 6, n = drafts_of(prm, b);
-    const double c = (double)(float)((double)prm.scale * kLog2e), dc = (double)(float)((double)prm.draft_scale * kLog2e);
-    for (int t = wave; t <= n; t += kWaves) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), b = blockIdx.x, n = drafts_of(prm, b);
+    const double c = (double)exponent_scale(prm.scale), dc = (double)exponent_scale(prm.draft_scale);
+    auto stats_of = [&](int64_t row, bool on) {
+        float2 mine = make_float2(kNegInf, 0.0f);
+        if (on && lane < cut.parts) mine = prm.stats[row * cut.parts + lane];
+        return mine;
+    };
+    for (int t = wave; t <= n; t += kDecideWaves) {
         const int64_t row = (int64_t)b * prm.q_len + t, draft_row = (int64_t)b * (prm.q_len - 1) + t;
-        const RowSum p = row_sum(prm.stats + row * cut.parts, cut.parts, lane);
+        const bool judges = t < n, with_draft = !kGreedy && judges && prm.draft;
+        const float2 mine = stats_of(row, true);
+        const float2 drafts = stats_of((int64_t)prm.batch * prm.q_len + draft_row, with_draft);
+        const int x = judges ? prm.draft_tokens[draft_row] : -1;
+        const bool is_token = x >= 0 && x < prm.vocab;
+        const double at = is_token ? logit_at<T>(prm.target, prm.target_stride, row, x) : 0.0;
+        const double draft_at = is_token && with_draft ? logit_at<T>(prm.draft, prm.draft_stride, draft_row, x) : 0.0;
+        const RowSum p = row_sum(mine);
+        const double lp = at * c - p.log2_sum;
+        double draft_top = 0.0;
         int best = -1;
-        if (prm.greedy) {
+        bool fine = false;
+        if constexpr (kGreedy) {
             uint64_t key = lane < cut.parts ? prm.best[row * cut.parts + lane] : 0;
 #pragma unroll
             for (int d = 1; d < 64; d *= 2) {
@@ -197,27 +244,16 @@ __device__ __forceinline__ Decision decide(const VerifyParams& prm, const Verify
                 key = other > key ? other : key;
             }
             best = (int)~(uint32_t)key;
-        }
-        bool fine = false;
-        double lp = 0.0, draft_top = 0.0;
-        int x = -1;
-        if (t < n) {
-            double lq = 0.0, draft_log2_sum = 0.0;
-            if (prm.draft && !prm.greedy) {
-                const RowSum q = row_sum(prm.stats + ((int64_t)prm.batch * prm.q_len + draft_row) * cut.parts, cut.parts, lane);
-                draft_log2_sum = q.log2_sum;
+            fine = judges && x == best && lp == lp;
+        } else if (judges) {
+            double lq = 0.0;
+            if (prm.draft) {
+                const RowSum q = row_sum(drafts);
                 draft_top = q.log2_sum - q.log2_sum == 0.0 ? q.top : __builtin_nan("");
+                lq = draft_at * dc - q.log2_sum;
             }
-            x = prm.draft_tokens[draft_row];
-            if (x >= 0 && x < prm.vocab) {
-                lp = logit_at<T>(prm.target, prm.target_stride, row, x) * c - p.log2_sum;
-                if (prm.greedy) {
-                    fine = x == best && lp == lp;
-                } else {
-                    if (prm.draft) lq = logit_at<T>(prm.draft, prm.draft_stride, draft_row, x) * dc - draft_log2_sum;
-                    fine = draft_top == draft_top && (double)prm.uniforms[(int64_t)b * prm.q_len + t] * exp2(lq) < exp2(lp);
-                }
-            }
+            // u q < p, where the row has probabilities: NaN and infinities are neither
+            fine = is_token && draft_top == draft_top && (double)prm.uniforms[row] * exp2_d(lq) < (lp == lp ? exp2_d(lp) : 0.0);
         }
         if (lane == 0) {
             lses[t] = p.log2_sum;
@@ -225,7 +261,7 @@ __device__ __forceinline__ Decision decide(const VerifyParams& prm, const Verify
             draft_tops[t] = draft_top;
             lps[t] = lp;
             stands[t] = fine;
-            tokens[t] = prm.greedy && (t == n || !fine) ? best : x;
+            tokens[t] = kGreedy && !fine ? best : x;
         }
     }
     __syncthreads();
@@ -236,27 +272,25 @@ __device__ __forceinline__ Decision decide(const VerifyParams& prm, const Verify
     d.top = tops[at];
     d.draft_top = draft_tops[at];
     d.row = lses[at] - lses[at] == 0.0 ? at : -1;
-    d.mode = prm.greedy || at == n || !(d.draft_top == d.draft_top) ? kPlain : prm.draft ? kRest : kWithout;
+    d.mode = kGreedy || at == n || !(d.draft_top == d.draft_top) ? kPlain : prm.draft ? kRest : kWithout;
     d.without = d.mode == kWithout && tokens[at] < prm.vocab ? tokens[at] : -1;
-    if (writes) {
-        if (tid < prm.q_len) {
-            int token = tid < at ? tokens[tid] : -1;
-            float lp = tid < at ? (float)(lps[tid] / kLog2e) : 0.0f;
-            if (prm.greedy && tid == at) {
-                token = d.row >= 0 ? tokens[at] : -1;
-                lp = d.row >= 0 ? (float)((logit_at<T>(prm.target, prm.target_stride, (int64_t)b * prm.q_len + at, token) * c - lses[at]) / kLog2e) : __builtin_nanf("");
-            }
-            prm.tokens[(int64_t)b * prm.q_len + tid] = token;
-            if (prm.token_lp) prm.token_lp[(int64_t)b * prm.q_len + tid] = lp;
+    if (tid < prm.q_len) {
+        int token = tid < at ? tokens[tid] : -1;
+        float lp = tid < at ? (float)(lps[tid] / kLog2e) : 0.0f;
+        if (kGreedy && tid == at) {
+            token = d.row >= 0 ? tokens[at] : -1;
+            lp = d.row >= 0 ? (float)((logit_at<T>(prm.target, prm.target_stride, (int64_t)b * prm.q_len + at, token) * c - lses[at]) / kLog2e) : __builtin_nanf("");
         }
-        if (tid == 0) {
-            prm.accepted[b] = at;
-            static_cast<Decision*>(prm.decisions)[b] = d;
-        }
+        prm.tokens[(int64_t)b * prm.q_len + tid] = token;
+        if (prm.token_lp) prm.token_lp[(int64_t)b * prm.q_len + tid] = lp;
     }
-    return d;
+    if (tid == 0) {
+        prm.accepted[b] = at;
+        if (!kGreedy) static_cast<Decision*>(prm.decisions)[b] = d;
+    }
 }
 
+// ---------------------------------------------------------------------------------- weigh
 // The rows that a sequence's new token comes from.
 template <typename T>
 struct Source {
@@ -276,7 +310,7 @@ __device__ __forceinline__ Source<T> source_of(const VerifyParams& prm, int b, c
 // Unnormalised weights of eight tokens.
 __device__ __forceinline__ void weights(const float (&x)[8], double c, double top, double (&w)[8]) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = x[j] == kNegInf ? 0.0 : exp2_d((double)x[j] * c - top);
+    for (int j = 0; j < 8; ++j) w[j] = exp2_d(__builtin_fma((double)x[j], c, -top));
 }
 
 __device__ __forceinline__ double block_sum_d(double x, int tid, double* space) {
@@ -288,26 +322,26 @@ __device__ __forceinline__ double block_sum_d(double x, int tid, double* space) 
     return all;
 }
 
-// grid.x = parts, grid.y = sequences.  The first part's workgroup leaves the decision for the passes behind.
+// grid.x = parts, grid.y = sequences.
 template <typename T>
-__global__ __launch_bounds__(kVerifyThreads) void verify_weigh_kernel(VerifyParams prm, VerifyCut read, VerifyCut cut) {
+__global__ __launch_bounds__(kVerifyThreads) void verify_weigh_kernel(VerifyParams prm, VerifyCut cut) {
     __shared__ double space[2][kWaves];
     const int tid = threadIdx.x, part = blockIdx.x, b = blockIdx.y;
-    const Decision d = decide<T>(prm, read, b, tid, part == 0);
-    if (d.row < 0 || prm.greedy) return;
+    const Decision d = static_cast<const Decision*>(prm.decisions)[b];
+    if (d.row < 0) return;
     const Source<T> s = source_of<T>(prm, b, d);
     const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
     double sum = 0.0, draft_sum = 0.0;
     for (int i = first + 8 * tid; i < end; i += kVerifyStep) {
-        float x[8];
+        float x[8], y[8];
         double w[8];
         load_logits(s.p + i, end - i, x);
+        if (s.q) load_logits(s.q + i, end - i, y);
         weights(x, s.c, d.top, w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum += i + j == d.without ? 0.0 : w[j];
         if (s.q) {
-            load_logits(s.q + i, end - i, x);
-            weights(x, s.dc, d.draft_top, w);
+            weights(y, s.dc, d.draft_top, w);
 #pragma unroll
             for (int j = 0; j < 8; ++j) draft_sum += w[j];
         }
@@ -333,12 +367,12 @@ __device__ __forceinline__ Norms norms_of(const VerifyParams& prm, const VerifyC
 // max(0, p - q) of eight tokens.
 template <typename T>
 __device__ __forceinline__ void rest_of(const Source<T>& s, const Decision& d, const Norms& norm, int i, int end, double (&w)[8]) {
-    float x[8];
+    float x[8], y[8];
     double v[8];
     load_logits(s.p + i, end - i, x);
+    load_logits(s.q + i, end - i, y);
     weights(x, s.c, d.top, w);
-    load_logits(s.q + i, end - i, x);
-    weights(x, s.dc, d.draft_top, v);
+    weights(y, s.dc, d.draft_top, v);
 #pragma unroll
     for (int j = 0; j < 8; ++j) w[j] = fmax(w[j] * norm.p - v[j] * norm.q, 0.0);
 }
@@ -363,130 +397,121 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_rest_kernel(VerifyParam
     if (tid == 0) prm.sums[((int64_t)2 * prm.batch + b) * cut.parts + part] = sum;
 }
 
-__device__ __forceinline__ double wave_scan_d(double x, int lane) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double other = __shfl_up(x, d, 64);
-        x += lane >= d ? other : 0.0;
-    }
-    return x;
-}
-
-// A workgroup per sequence: the part that holds the random number's share of the sum, then step by step the logits of that part.
+// A workgroup per sequence: the part that holds the random number's share of the sum, then step by step the logits of that part.  Bound by the
+// fetching of its own instructions, each of which it needs once: four logits per thread (of 512) instead of eight.
+constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64, kPickLogits = kVerifyStep / kPickThreads;
 template <typename T>
-__global__ __launch_bounds__(kVerifyThreads) void verify_pick_kernel(VerifyParams prm, VerifyCut read, VerifyCut cut) {
-    __shared__ double totals[kWaves];
-    __shared__ int found, last;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x;
+__global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams prm, VerifyCut cut) {
+    __shared__ double totals[kPickWaves];
+    __shared__ int tops[kPickWaves], heres[kPickWaves];      // a wave's last token with a weight, and the first beyond the goal
+    const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), b = blockIdx.x;
+    const double u = (double)prm.uniforms[(int64_t)b * prm.q_len + prm.q_len - 1];
+    double part_sums[3];      // all that may be needed, in one round trip
+#pragma unroll
+    for (int k = 0; k < 3; ++k) part_sums[k] = lane < cut.parts && (k < 2 || prm.draft) ? prm.sums[((int64_t)k * prm.batch + b) * cut.parts + lane] : 0.0;
     const Decision d = static_cast<const Decision*>(prm.decisions)[b];
+    constexpr int kNone = 0x7fffffff;
+    int last = -1;
     const int64_t out = (int64_t)b * prm.q_len + d.accepted;
-    auto nothing = [&] {
+    const double upto_p = wave_scan_d(part_sums[0]), all_p = lane_d(upto_p, 63);
+    const Norms norm = {1.0 / all_p, 1.0 / wave_sum_d(part_sums[1])};
+    const double upto_rest = wave_scan_d(part_sums[2]), all_rest = lane_d(upto_rest, 63);
+    // p nowhere above q: nothing could have fallen but by rounding
+    const bool rest = d.row >= 0 && d.mode == kRest && all_rest > 0.0;
+    const double all = rest ? all_rest : all_p, upto = rest ? upto_rest : upto_p, mine = rest ? part_sums[2] : part_sums[0];
+    if (d.row < 0 || !(all > 0.0) || !(all < __builtin_inf())) {
         if (tid == 0) {
-            prm.tokens[out] = -1;
-            if (prm.token_lp) prm.token_lp[out] = __builtin_nanf("");
+            // without a token that has all of p, it comes back: rounding alone let it fall
+            const bool back = d.row >= 0 && d.mode == kWithout;
+            prm.tokens[out] = back ? d.without : -1;
+            if (prm.token_lp) prm.token_lp[out] = back ? 0.0f : __builtin_nanf("");
         }
-    };
-    if (d.row < 0) {
-        nothing();
         return;
     }
     const Source<T> s = source_of<T>(prm, b, d);
-    const Norms norm = norms_of(prm, cut, b, lane);
-    bool rest = d.mode == kRest;
-    double mine = lane < cut.parts ? prm.sums[((int64_t)(rest ? 2 : 0) * prm.batch + b) * cut.parts + lane] : 0.0;
-    double upto = wave_scan_d(mine, lane), all = __shfl(upto, 63, 64);
-    if (rest && !(all > 0.0)) {      // p is nowhere above q: nothing could have fallen but by rounding
-        rest = false;
-        mine = lane < cut.parts ? prm.sums[(int64_t)b * cut.parts + lane] : 0.0;
-        upto = wave_scan_d(mine, lane);
-        all = __shfl(upto, 63, 64);
-    }
-    if (!(all > 0.0) && d.mode == kWithout) {      // the token left out has all of p: rounding alone let it fall
-        if (tid == 0) {
-            prm.tokens[out] = d.without;
-            if (prm.token_lp) prm.token_lp[out] = 0.0f;
+    auto finish = [&](int token, double logit) {
+        prm.tokens[out] = token;
+        if (prm.token_lp) {
+            double z = all_p;      // without the token left out
+            const double less = d.without < 0 ? (double)kNegInf : (double)to_float(s.p[d.without]);
+            if (less > kNegInf) z += exp2_d(less * s.c - d.top);
+            prm.token_lp[out] = (float)((logit * s.c - d.top - log2_d(z)) / kLog2e);
         }
-        return;
-    }
-    if (!(all > 0.0) || !(all < __builtin_inf())) {
-        nothing();
-        return;
-    }
-    const double u = (double)prm.uniforms[(int64_t)b * prm.q_len + prm.q_len - 1], goal = u * all;
+    };
+    const double goal = u * all;
     const unsigned long long hit = __ballot(lane < cut.parts && upto > goal), some = __ballot(mine > 0.0);
-    const int part = hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(some);
-    double before = __shfl(upto - mine, part, 64);
+    const int part = uniform(hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(some));
+    double before = lane_d(upto - mine, part);
     const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
-    if (tid == 0) {
-        found = 0x7fffffff;
-        last = -1;
-    }
     for (int step = first; step < end; step += kVerifyStep) {
-        const int i = step + 8 * tid;
-        double w[8] = {};
-        if (i < end) {
-            if (rest) {
-                rest_of(s, d, norm, i, end, w);
-            } else {
-                float x[8];
-                load_logits(s.p + i, end - i, x);
-                weights(x, s.c, d.top, w);
+        const int i = step + kPickLogits * tid;
+        float x[kPickLogits], y[kPickLogits];
+        double w[kPickLogits];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) w[j] = i + j == d.without ? 0.0 : w[j];
-            }
+        for (int j = 0; j < kPickLogits; ++j) {
+            x[j] = i + j < end ? to_float(s.p[i + j]) : kNegInf;
+            y[j] = rest && i + j < end ? to_float(s.q[i + j]) : kNegInf;
         }
         double sum = 0.0;
         int top = -1;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < kPickLogits; ++j) {
+            w[j] = i + j == d.without ? 0.0 : exp2_d(__builtin_fma((double)x[j], s.c, -d.top));
+            if (rest) w[j] = fmax(w[j] * norm.p - exp2_d(__builtin_fma((double)y[j], s.dc, -d.draft_top)) * norm.q, 0.0);
             sum += w[j];
             top = w[j] > 0.0 ? i + j : top;
         }
-        const double scan = wave_scan_d(sum, lane);
-        __syncthreads();
-        if (lane == 63) totals[wave] = scan;
-        if (top >= 0) atomicMax(&last, top);
+        const double scan = wave_scan_d(sum);
+        const unsigned long long with = __ballot(top >= 0);
+        top = with ? __builtin_amdgcn_readlane(top, 63 - __builtin_clzll(with | 1)) : -1;
+        __syncthreads();      // the step before has been read
+        if (lane == 63) {
+            totals[wave] = scan;
+            tops[wave] = top;
+        }
         __syncthreads();
         double at = before + (scan - sum);
-        for (int q = 0; q < kWaves; ++q) {
+        for (int q = 0; q < kPickWaves; ++q) {
             at += q < wave ? totals[q] : 0.0;
             before += totals[q];
+            last = tops[q] > last ? tops[q] : last;
         }
-        int here = 0x7fffffff;
+        int here = kNone;
+        float logit = 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
+        for (int j = 0; j < kPickLogits; ++j) {
             at += w[j];
-            if (at > goal && w[j] > 0.0 && here == 0x7fffffff) here = i + j;
+            const bool is = at > goal && w[j] > 0.0 && here == kNone;
+            logit = is ? x[j] : logit;
+            here = is ? i + j : here;
         }
-        if (here != 0x7fffffff) atomicMin(&found, here);
+        const unsigned long long beyond = __ballot(here != kNone);
+        const int first_here = __builtin_amdgcn_readlane(here, beyond ? __builtin_ctzll(beyond) : 0);
+        if (lane == 0) heres[wave] = first_here;
         __syncthreads();
-        if (found != 0x7fffffff) break;
+        int found = kNone;
+        for (int q = 0; q < kPickWaves; ++q) found = heres[q] < found ? heres[q] : found;
+        if (found == kNone) continue;
+        if (here == found) finish(here, (double)logit);
+        return;
     }
-    if (tid == 0) {
-        const int token = found != 0x7fffffff ? found : last;      // the last of the part where rounding leaves the goal just behind it
-        prm.tokens[out] = token;
-        if (prm.token_lp) {
-            double z = 0.0;
-            for (int q = 0; q < cut.parts; ++q) z += prm.sums[(int64_t)b * cut.parts + q];
-            if (d.mode == kWithout) {      // the sums lack the token left out
-                const double less = d.without < 0 ? (double)kNegInf : (double)to_float(s.p[d.without]);
-                if (less > kNegInf) z += exp2_d(less * s.c - d.top);
-            }
-            prm.token_lp[out] = (float)(((double)to_float(s.p[token]) * s.c - d.top - log2(z)) / kLog2e);
-        }
-    }
+    if (tid == 0) finish(last, (double)to_float(s.p[last]));      // the part's last one, where rounding leaves the goal just behind it
 }
 
+template <typename T, bool kGreedy>
+hipError_t launch_first(const VerifyParams& prm, const VerifyLayout& w, hipStream_t stream) {
+    const long rows = (long)prm.batch * (prm.draft ? 2 * prm.q_len - 1 : prm.q_len);
+    const hipError_t e = launch(verify_read_kernel<T, kGreedy>, dim3((unsigned)rows, (unsigned)w.read.parts), kVerifyThreads, stream, prm, w.read);
+    return e != hipSuccess ? e : launch(verify_decide_kernel<T, kGreedy>, dim3((unsigned)prm.batch), 64 * kDecideWaves, stream, prm, w.read);
+}
 template <typename T>
 hipError_t launch_type(const VerifyParams& prm, const VerifyLayout& w, hipStream_t stream) {
-    const long rows = (long)prm.batch * (prm.draft && !prm.greedy ? 2 * prm.q_len - 1 : prm.q_len);
-    hipError_t e = launch(verify_read_kernel<T>, dim3((unsigned)rows, (unsigned)w.read.parts), kVerifyThreads, stream, prm, w.read);
-    if (e != hipSuccess) return e;
-    const dim3 grid(prm.greedy ? 1u : (unsigned)w.pick.parts, (unsigned)prm.batch);
-    e = launch(verify_weigh_kernel<T>, grid, kVerifyThreads, stream, prm, w.read, w.pick);
-    if (e != hipSuccess || prm.greedy) return e;
-    if (prm.draft && (e = launch(verify_rest_kernel<T>, grid, kVerifyThreads, stream, prm, w.pick)) != hipSuccess) return e;
-    return launch(verify_pick_kernel<T>, dim3((unsigned)prm.batch), kVerifyThreads, stream, prm, w.read, w.pick);
+    if (prm.greedy) return launch_first<T, true>(prm, w, stream);
+    const dim3 grid((unsigned)w.pick.parts, (unsigned)prm.batch);
+    hipError_t e = launch_first<T, false>(prm, w, stream);
+    if (e == hipSuccess) e = launch(verify_weigh_kernel<T>, grid, kVerifyThreads, stream, prm, w.pick);
+    if (e == hipSuccess && prm.draft) e = launch(verify_rest_kernel<T>, grid, kVerifyThreads, stream, prm, w.pick);
+    return e != hipSuccess ? e : launch(verify_pick_kernel<T>, dim3((unsigned)prm.batch), kPickThreads, stream, prm, w.pick);
 }
 
 }  // namespace
