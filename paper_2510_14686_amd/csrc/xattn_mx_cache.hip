@@ -37,10 +37,31 @@ __device__ __forceinline__ double block_max(double x) {
     x = fmax(x, dpp_d<0xB1>(x));
     return fmax(x, dpp_d<0x4E>(x));
 }
+__device__ __forceinline__ uint32_t block_max(uint32_t x) {
+    const uint32_t y = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0xB1, 0xf, 0xf, true);
+    x = x > y ? x : y;
+    const uint32_t z = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x4E, 0xf, 0xf, true);
+    return x > z ? x : z;
+}
 
-// Eight values of a block as codes, and the block's scale byte.  Called by the block's four lanes.  The values come in double, since their last
-// bit can decide a code; a float with the rest of the digits in its last bit rounds the same way.
-__device__ __forceinline__ uint32_t encode(const double (&x)[8], int& scale_byte) {
+// Eight values of a block as codes, and the block's scale byte.  Called by the block's four lanes.
+struct Encoded {
+    uint32_t codes;
+    int scale;
+};
+// The exponent of the scale, of the largest value's: 1.f * 2^e is within 7 * 2^(e - 2) up to 1.75 * 2^e.
+__device__ __forceinline__ int scale_exp(int e, bool above) {
+    e += above ? -1 : -2;
+    return e < kMxLeastExp ? kMxLeastExp : e > kMxMostExp ? kMxMostExp : e;
+}
+__device__ __forceinline__ uint32_t convert(const float (&f)[8], float scale) {
+    uint32_t codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, f[0], f[1], scale, 0);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], scale, 1);
+    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], scale, 2);
+    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], scale, 3);
+}
+// Rotated values in double, whose last bit can decide a code: a float with whether anything was cut off in its last bit rounds the same way.
+__device__ __forceinline__ Encoded encode(const double (&x)[8]) {
     double most = 0.0;
     bool finite = true;
 #pragma unroll
@@ -51,22 +72,34 @@ __device__ __forceinline__ uint32_t encode(const double (&x)[8], int& scale_byte
     }
     most = block_max(finite ? most : __builtin_inf());
     const uint64_t bits = __builtin_bit_cast(uint64_t, most);
-    int e = (int)(bits >> 52) - 1023 - 2 + ((bits & 0xfffffffffffffull) > 0xc000000000000ull ? 1 : 0);
-    e = e < kMxLeastExp ? kMxLeastExp : e > kMxMostExp ? kMxMostExp : e;
-    scale_byte = most < __builtin_inf() ? e + 127 : kMxNanScale;
+    const int e = scale_exp((int)(bits >> 52) - 1023, (bits & 0xfffffffffffffull) > 0xc000000000000ull);
     const double up = __builtin_bit_cast(double, (uint64_t)(1023 - e) << 52);
-    uint32_t codes = 0;
     float f[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+        // the 29 lowest bits of the significand cut off, what is left is a float's (or less than its least normal number, far below half a code)
         const double y = x[i] * up;
-        const float t = __double2float_rz(y);
-        f[i] = __uint_as_float(__float_as_uint(t) | ((double)t != y ? 1u : 0u));
+        const uint64_t u = __builtin_bit_cast(uint64_t, y);
+        const double cut = __builtin_bit_cast(double, u & ~0x1fffffffull);
+        f[i] = __uint_as_float(__float_as_uint((float)cut) | (((uint32_t)u & 0x1fffffffu) != 0u ? 1u : 0u));
     }
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[0], f[1], 1.0f, 0);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[2], f[3], 1.0f, 1);
-    codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[4], f[5], 1.0f, 2);
-    return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6], f[7], 1.0f, 3);
+    return Encoded{convert(f, 1.0f), most < __builtin_inf() ? e + 127 : kMxNanScale};
+}
+// Eight bf16 as they are.
+__device__ __forceinline__ Encoded encode(u32x4_t x) {
+    uint32_t most = 0;      // the sizes order as their bits do; NaN and infinities are the largest
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t lo = x[i] & 0x7fffu, hi = x[i] >> 16 & 0x7fffu;
+        most = lo > most ? lo : most;
+        most = hi > most ? hi : most;
+        f[2 * i] = bf16_lo(x[i]);
+        f[2 * i + 1] = bf16_hi(x[i]);
+    }
+    most = block_max(most);
+    const int e = scale_exp((int)(most >> 7) - 127, (most & 0x7fu) > 0x60u);
+    return Encoded{convert(f, __uint_as_float((uint32_t)(e + 127) << 23)), most < 0x7f80u ? e + 127 : kMxNanScale};
 }
 
 __device__ __forceinline__ void widen(u32x4_t x, double (&d)[8]) {
@@ -75,6 +108,13 @@ __device__ __forceinline__ void widen(u32x4_t x, double (&d)[8]) {
         d[2 * i] = (double)bf16_lo(x[i]);
         d[2 * i + 1] = (double)bf16_hi(x[i]);
     }
+}
+// What the lane eight further in its row of 16 holds.
+__device__ __forceinline__ u32x4_t across(u32x4_t x) {
+    u32x4_t y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x[i], 0x128, 0xf, 0xf, true);      // row_ror:8
+    return y;
 }
 
 template <int kTokens>
@@ -85,7 +125,58 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
     __shared__ char* bases[kTokens][2];
     __shared__ int known[kTokens];              // whether a sequence has it
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6));
-    const int token0 = blockIdx.x * kTokens, F = prm.frequencies;
+    const int token0 = blockIdx.x * kTokens, F = prm.frequencies, turned = F / 8;
+    const bool halves = F == kPairs && !prm.pairs;      // value i turns with value 64 + i: another lane of the head has it
+    // q: 16 values of a head at a time, in two pieces
+    const int q_items = prm.n_q_heads * (kHeadDim / 16);
+    struct QItem {
+        int tk, at0, at1, c;
+        bool turn;
+        int64_t at;
+        u32x4_t x, y;
+    };
+    auto fetch_q = [&](int item) {
+        QItem r;
+        r.tk = kTokens == 1 ? 0 : (int)((unsigned)item / (unsigned)q_items);
+        const int rest = item - r.tk * q_items, head = rest >> 3;
+        r.c = rest & 7;
+        const int64_t row = token0 + r.tk < prm.total_q ? token0 + r.tk : prm.total_q - 1;
+        r.turn = r.c < turned;
+        const bool apart = r.turn && !prm.pairs;
+        r.at0 = apart ? 8 * r.c : 16 * r.c;
+        r.at1 = apart ? F + 8 * r.c : 16 * r.c + 8;
+        r.at = (row * prm.n_q_heads + head) * kHeadDim;
+        const uint16_t* const from = prm.q + row * prm.q_stride + head * kHeadDim;
+        r.x = *reinterpret_cast<const u32x4_t*>(from + r.at0);
+        r.y = *reinterpret_cast<const u32x4_t*>(from + r.at1);
+        return r;
+    };
+    // k and v: 8 values of a head at a time, 16 lanes a head
+    const int kv_items = prm.n_kv_heads * 16;
+    struct KvItem {
+        int tk, head, m;
+        bool is_v, second;
+        u32x4_t x, other;
+    };
+    auto fetch_kv = [&](int item) {
+        KvItem r;
+        const int tk2 = (int)((unsigned)item / (unsigned)kv_items), rest = item - tk2 * kv_items;
+        r.tk = tk2 >> 1;
+        r.is_v = (tk2 & 1) != 0;
+        r.head = rest >> 4;
+        r.m = rest & 15;
+        r.second = 8 * r.m >= F;
+        const int64_t row = token0 + r.tk < prm.total_q ? token0 + r.tk : prm.total_q - 1;
+        const uint16_t* const from = (r.is_v ? prm.v + row * prm.v_stride : prm.k + row * prm.k_stride) + r.head * kHeadDim;
+        r.x = *reinterpret_cast<const u32x4_t*>(from + 8 * r.m);
+        r.other = r.x;
+        if (!halves && !prm.pairs && !r.is_v && r.m < 2 * turned) r.other = *reinterpret_cast<const u32x4_t*>(from + (r.second ? 8 * r.m - F : 8 * r.m + F));
+        return r;
+    };
+    // The first of each are on their way while the rows' sequences are looked for and the angles worked out.
+    const int q_all = kTokens * q_items, kv_all = 2 * kTokens * kv_items, tid = threadIdx.x;
+    QItem next_q = fetch_q(tid < q_all ? tid : 0);
+    KvItem next_kv = fetch_kv(tid < kv_all ? tid : 0);
     if (wave < kTokens) {
         const int row = token0 + wave;
         int start = 0, end = 0;
@@ -110,22 +201,17 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
     }
     __syncthreads();
 
-    // q: 16 values of a head at a time, in two pieces
-    const int q_items = prm.n_q_heads * (kHeadDim / 16), turned = F / 8;
-    for (int item = threadIdx.x; item < kTokens * q_items; item += kRopeThreads) {
-        const int tk = item / q_items, rest = item - tk * q_items, head = rest >> 3, c = rest & 7;
-        if (!known[tk]) continue;
-        const int64_t row = token0 + tk;
-        const bool turn = c < turned, apart = turn && !prm.pairs;
-        const int at0 = apart ? 8 * c : 16 * c, at1 = apart ? F + 8 * c : 16 * c + 8;
-        const uint16_t* const from = prm.q + row * prm.q_stride + head * kHeadDim;
-        u32x4_t x = *reinterpret_cast<const u32x4_t*>(from + at0), y = *reinterpret_cast<const u32x4_t*>(from + at1);
-        if (turn) {
+    for (int item = tid; item < q_all; item += kRopeThreads) {
+        QItem it = next_q;
+        if (item + kRopeThreads < q_all) next_q = fetch_q(item + kRopeThreads);
+        if (!known[it.tk]) continue;
+        u32x4_t &x = it.x, &y = it.y;
+        if (it.turn) {
             float co[8], si[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                co[i] = (float)cosines[tk][8 * c + i];
-                si[i] = (float)sines[tk][8 * c + i];
+                co[i] = (float)cosines[it.tk][8 * it.c + i];
+                si[i] = (float)sines[it.tk][8 * it.c + i];
             }
             if (prm.pairs) {
 #pragma unroll
@@ -143,84 +229,105 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
                 }
             }
         }
-        uint16_t* const to = prm.q_out + (row * prm.n_q_heads + head) * kHeadDim;
-        *reinterpret_cast<u32x4_t*>(to + at0) = x;
-        *reinterpret_cast<u32x4_t*>(to + at1) = y;
+        *reinterpret_cast<u32x4_t*>(prm.q_out + it.at + it.at0) = x;
+        *reinterpret_cast<u32x4_t*>(prm.q_out + it.at + it.at1) = y;
     }
 
-    // k and v: 8 values of a head at a time, 16 lanes a head
-    const int kv_items = prm.n_kv_heads * 16;
-    for (int item = threadIdx.x; item < 2 * kTokens * kv_items; item += kRopeThreads) {
-        const int tk2 = item / kv_items, rest = item - tk2 * kv_items, head = rest >> 4, m = rest & 15, tk = tk2 >> 1;
-        const bool is_v = (tk2 & 1) != 0;
-        if (!known[tk] || places[tk] < 0) continue;
-        const int64_t row = token0 + tk;
-        const uint16_t* const from = (is_v ? prm.v + row * prm.v_stride : prm.k + row * prm.k_stride) + head * kHeadDim;
-        double x[8];
-        widen(*reinterpret_cast<const u32x4_t*>(from + 8 * m), x);
-        if (!is_v && 8 * m < 2 * F) {
-            if (prm.pairs) {
+    for (int item = tid; item < kv_all; item += kRopeThreads) {
+        const KvItem it = next_kv;
+        if (item + kRopeThreads < kv_all) next_kv = fetch_kv(item + kRopeThreads);
+        if (!known[it.tk] || places[it.tk] < 0) continue;
+        Encoded e;
+        MxPlace to;
+        if (it.is_v) {
+            e = encode(it.x);
+            to = mx_place<true>(places[it.tk], it.head, prm.n_kv_heads, it.m);
+        } else {
+            double x[8];
+            widen(it.x, x);
+            if (it.m < 2 * turned) {
+                if (prm.pairs) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const double co = cosines[tk][4 * m + i], si = sines[tk][4 * m + i], a = x[2 * i], b = x[2 * i + 1];
-                    x[2 * i] = a * co - b * si;
-                    x[2 * i + 1] = b * co + a * si;
-                }
-            } else {
-                const bool second = 8 * m >= F;
-                const int first = second ? 8 * m - F : 8 * m;
-                double other[8];
-                widen(*reinterpret_cast<const u32x4_t*>(from + (second ? 8 * m - F : 8 * m + F)), other);
+                    for (int i = 0; i < 4; ++i) {
+                        const double co = cosines[it.tk][4 * it.m + i], si = sines[it.tk][4 * it.m + i], a = x[2 * i], b = x[2 * i + 1];
+                        x[2 * i] = a * co - b * si;
+                        x[2 * i + 1] = b * co + a * si;
+                    }
+                } else {
+                    const int first = it.second ? 8 * it.m - F : 8 * it.m;
+                    double other[8];
+                    widen(halves ? across(it.x) : it.other, other);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const double co = cosines[tk][first + i], si = sines[tk][first + i];
-                    x[i] = second ? x[i] * co + other[i] * si : x[i] * co - other[i] * si;
+                    for (int i = 0; i < 8; ++i) {
+                        const double co = cosines[it.tk][first + i], si = sines[it.tk][first + i];
+                        x[i] = x[i] * co + other[i] * (it.second ? si : -si);
+                    }
                 }
             }
+            e = encode(x);
+            to = mx_place<false>(places[it.tk], it.head, prm.n_kv_heads, it.m);
         }
-        int scale;
-        const uint32_t codes = encode(x, scale);
-        const MxPlace to = is_v ? mx_place<true>(places[tk], head, prm.n_kv_heads, m) : mx_place<false>(places[tk], head, prm.n_kv_heads, m);
-        char* const base = bases[tk][is_v ? 1 : 0];
-        *reinterpret_cast<uint32_t*>(base + to.codes) = codes;
-        if ((m & 3) == 0) *reinterpret_cast<uint8_t*>(base + to.scale) = (uint8_t)scale;
+        char* const base = bases[it.tk][it.is_v ? 1 : 0];
+        *reinterpret_cast<uint32_t*>(base + to.codes) = e.codes;
+        if ((it.m & 3) == 0) *reinterpret_cast<uint8_t*>(base + to.scale) = (uint8_t)e.scale;
     }
 }
 
-// A workgroup takes 16 rows of one head, 16 lanes a row: rows that follow each other share the lines of the cache.
-constexpr int kReadRows = 16;
+// A wave takes four rows, 16 lanes a row, of all heads: a row's sequence is looked for once, and rows that follow each other share the lines of
+// the cache.
+constexpr int kReadRows = 16, kReadHeads = 4, kReadFewRows = 2048;
 __global__ __launch_bounds__(256) void read_mx_kernel(ReadMxParams prm) {
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), m = lane & 15;
-    const int head = blockIdx.y, row0 = blockIdx.x * kReadRows + 4 * wave;
-    int start = 0, end = 0, b = -1;
+    const int row0 = blockIdx.x * kReadRows + 4 * wave;
+    int start = 0, end = 0, b = -1, at = -1;      // at: the lane's row in its sequence, -1 where that would be negative, -2 without a sequence
+    const char *kp = nullptr, *vp = nullptr;
     for (int i = 0; i < 4; ++i) {
         const int row = row0 + i;
-        if (row >= prm.total_q) return;
-        if (b < 0 || row < start || row >= end) b = find_sequence(prm.q_starts, prm.batch, row, lane, start, end);
-        if (b < 0) continue;
-        const int len = prm.kv_lens[b];
-        if (lane >> 4 != i) continue;
-        u32x4_t k = {0u, 0u, 0u, 0u}, v = {0u, 0u, 0u, 0u};
-        if (len >= end - row) {
-            const int at = len - (end - row);
-            const char* const kp = static_cast<const char*>(prm.k_ptrs[b]);
-            const char* const vp = static_cast<const char*>(prm.v_ptrs[b]);
-            const MxPlace pk = mx_place<false>(at, head, prm.n_kv_heads, m), pv = mx_place<true>(at, head, prm.n_kv_heads, m);
-            const uint32_t kc = *reinterpret_cast<const uint32_t*>(kp + pk.codes), vc = *reinterpret_cast<const uint32_t*>(vp + pv.codes);
-            const float ks = __uint_as_float((uint32_t)*reinterpret_cast<const uint8_t*>(kp + pk.scale) << 23);
-            const float vs = __uint_as_float((uint32_t)*reinterpret_cast<const uint8_t*>(vp + pv.scale) << 23);
-            auto unpack = [](uint32_t codes, float scale) {
-                return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0)),
-                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1)),
-                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2)),
-                               __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3))};
-            };
-            k = unpack(kc, ks);
-            v = unpack(vc, vs);
+        if (b < 0 || row >= end) b = row < prm.total_q ? find_sequence(prm.q_starts, prm.batch, row, lane, start, end) : -1;
+        int place = -2;
+        const char *k = nullptr, *v = nullptr;
+        if (b >= 0) {
+            const int len = prm.kv_lens[b];
+            place = len >= end - row ? len - (end - row) : -1;
+            k = static_cast<const char*>(prm.k_ptrs[b]);
+            v = static_cast<const char*>(prm.v_ptrs[b]);
         }
-        const int64_t to = ((int64_t)row * prm.n_kv_heads + head) * kHeadDim + 8 * m;
-        *reinterpret_cast<u32x4_t*>(prm.k_out + to) = k;
-        *reinterpret_cast<u32x4_t*>(prm.v_out + to) = v;
+        if (lane >> 4 == i) {
+            at = place;
+            kp = k;
+            vp = v;
+        }
+    }
+    if (at == -2) return;
+    const MxPlace pk = mx_place<false>(at < 0 ? 0 : at, 0, prm.n_kv_heads, m), pv = mx_place<true>(at < 0 ? 0 : at, 0, prm.n_kv_heads, m);
+    auto unpack = [](uint32_t codes, uint32_t scale) {
+        const float s = __uint_as_float(scale << 23);
+        return u32x4_t{__builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 0)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 1)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 2)),
+                       __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, s, 3))};
+    };
+    const int64_t to = ((int64_t)(row0 + (lane >> 4)) * prm.n_kv_heads) * kHeadDim + 8 * m;
+    for (int head0 = blockIdx.y * kReadHeads; head0 < prm.n_kv_heads; head0 += kReadHeads * gridDim.y) {
+        uint32_t kc[kReadHeads], vc[kReadHeads], ks[kReadHeads], vs[kReadHeads];
+#pragma unroll
+        for (int h = 0; h < kReadHeads; ++h) {
+            const bool on = head0 + h < prm.n_kv_heads && at >= 0;
+            const int64_t tile = (int64_t)(head0 + h) * kMxTileBytes;
+            kc[h] = vc[h] = ks[h] = vs[h] = 0;
+            if (on) {
+                kc[h] = *reinterpret_cast<const uint32_t*>(kp + pk.codes + tile);
+                ks[h] = *reinterpret_cast<const uint8_t*>(kp + pk.scale + tile);
+                vc[h] = *reinterpret_cast<const uint32_t*>(vp + pv.codes + tile);
+                vs[h] = *reinterpret_cast<const uint8_t*>(vp + pv.scale + tile);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < kReadHeads; ++h) {
+            if (head0 + h >= prm.n_kv_heads) break;
+            *reinterpret_cast<u32x4_t*>(prm.k_out + to + (head0 + h) * kHeadDim) = unpack(kc[h], ks[h]);
+            *reinterpret_cast<u32x4_t*>(prm.v_out + to + (head0 + h) * kHeadDim) = unpack(vc[h], vs[h]);
+        }
     }
 }
 
@@ -239,7 +346,9 @@ hipError_t launch_rope_mx(const RopeParams& prm, hipStream_t stream) {
 }
 
 hipError_t launch_read_mx(const ReadMxParams& prm, hipStream_t stream) {
-    return launch(read_mx_kernel, dim3((unsigned)((prm.total_q + kReadRows - 1) / kReadRows), (unsigned)prm.n_kv_heads), 256, stream, prm);
+    // Few rows: heads go to workgroups of their own.
+    const int rows = (prm.total_q + kReadRows - 1) / kReadRows, heads = (prm.n_kv_heads + kReadHeads - 1) / kReadHeads;
+    return launch(read_mx_kernel, dim3((unsigned)rows, rows < kReadFewRows ? (unsigned)heads : 1u), 256, stream, prm);
 }
 
 }  // namespace xattn
