@@ -62,15 +62,13 @@ __device__ __forceinline__ uint32_t convert(const float (&f)[8], float scale) {
 }
 // Rotated values in double, whose last bit can decide a code: a float with whether anything was cut off in its last bit rounds the same way.
 __device__ __forceinline__ Encoded encode(const double (&x)[8]) {
-    double most = 0.0;
-    bool finite = true;
+    double most = 0.0, zero = 0.0;      // zero: NaN where a value is no number or infinite
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const double a = fabs(x[i]);
-        finite = finite && a < __builtin_inf();
-        most = fmax(most, a);
+        most = fmax(most, fabs(x[i]));
+        zero = __builtin_fma(x[i], 0.0, zero);
     }
-    most = block_max(finite ? most : __builtin_inf());
+    most = block_max(zero == 0.0 ? most : __builtin_inf());
     const uint64_t bits = __builtin_bit_cast(uint64_t, most);
     const int e = scale_exp((int)(bits >> 52) - 1023, (bits & 0xfffffffffffffull) > 0xc000000000000ull);
     const double up = __builtin_bit_cast(double, (uint64_t)(1023 - e) << 52);
@@ -120,7 +118,8 @@ __device__ __forceinline__ u32x4_t across(u32x4_t x) {
 template <int kTokens>
 __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
     constexpr int kPairs = kHeadDim / 2;
-    __shared__ double cosines[kTokens][kPairs], sines[kTokens][kPairs];
+    __shared__ double cosines[kTokens][kPairs], sines[kTokens][kPairs];      // for k, whose codes take all digits
+    __shared__ __attribute__((aligned(16))) float q_cosines[kTokens][kPairs], q_sines[kTokens][kPairs];
     __shared__ int places[kTokens];             // row of the cache, or -1
     __shared__ char* bases[kTokens][2];
     __shared__ int known[kTokens];              // whether a sequence has it
@@ -195,6 +194,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
                 sincospi(2.0 * ((turns - rint(turns)) + rest), &sine, &cosine);
                 cosines[wave][i] = cosine;
                 sines[wave][i] = sine;
+                q_cosines[wave][i] = (float)cosine;
+                q_sines[wave][i] = (float)sine;
             }
         }
         if (lane == 0) known[wave] = b >= 0;
@@ -210,8 +211,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
             float co[8], si[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                co[i] = (float)cosines[it.tk][8 * it.c + i];
-                si[i] = (float)sines[it.tk][8 * it.c + i];
+                co[i] = q_cosines[it.tk][8 * it.c + i];
+                si[i] = q_sines[it.tk][8 * it.c + i];
             }
             if (prm.pairs) {
 #pragma unroll
@@ -255,13 +256,10 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
                     }
                 } else {
                     const int first = it.second ? 8 * it.m - F : 8 * it.m;
-                    double other[8];
-                    widen(halves ? across(it.x) : it.other, other);
+                    double other[8];      // with the sign of the sine's product: a first half's is subtracted
+                    widen((halves ? across(it.x) : it.other) ^ (it.second ? 0u : 0x80008000u), other);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        const double co = cosines[it.tk][first + i], si = sines[it.tk][first + i];
-                        x[i] = x[i] * co + other[i] * (it.second ? si : -si);
-                    }
+                    for (int i = 0; i < 8; ++i) x[i] = x[i] * cosines[it.tk][first + i] + other[i] * sines[it.tk][first + i];
                 }
             }
             e = encode(x);
