@@ -408,7 +408,7 @@ int xattn_rope_kvcache(const void* q, const void* k_new, const void* v_new, int6
  *                        as they were.  (A prompt's chunk behind a cached part: read all rows, attend them with xattn_prefill.)
  *                        Bounds and limits as for xattn_rope_kvcache.
  * xattn_decode_mx        xattn_decode over such ranges: same arguments, shapes, masks, outputs, stream, capture and ownership rules, and the
- *                        same workspace, of at least xattn_decode_mx_workspace_bytes.  scale * log2 e finite.  K and V enter the products
+ *                        same workspace, of at least xattn_decode_mx_workspace_bytes.  scale * log2 e finite, up to 1024 KV heads.  K and V enter the products
  *                        exactly; scores, maxima and sums are fp32; a softmax weight enters the value product as two bf16 (16 significant bits).
  *                        A NaN or an infinity in a sequence's rows or queries leaves its results unspecified, and no others.  XATTN_CFG_* do not apply.
  */

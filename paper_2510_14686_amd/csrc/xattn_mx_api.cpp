@@ -14,6 +14,7 @@ namespace xattn {
 
 namespace {
 
+constexpr int kMxMaxHeads = 1024;
 constexpr int kMaxVerifyBatch = 4096, kMaxVerifyQLen = 16, kMaxVerifyVocab = 1 << 24;
 
 bool misaligned(const void* p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to != 0; }
@@ -46,7 +47,7 @@ size_t xattn_mx_range_bytes(int64_t tokens, int n_kv_heads, int head_dim) {
         fail(XATTN_EINVAL, "%s: tokens must not be negative, n_kv_heads and head_dim must be positive", who);
         return 0;
     }
-    if (head_dim != kHeadDim || n_kv_heads > 1024 || tokens > INT32_MAX) {
+    if (head_dim != kHeadDim || n_kv_heads > kMxMaxHeads || tokens > INT32_MAX) {
         fail(XATTN_EUNSUPPORTED, "%s: head_dim 128, up to 1024 heads and 2^31 - 1 tokens are supported", who);
         return 0;
     }
@@ -55,6 +56,10 @@ size_t xattn_mx_range_bytes(int64_t tokens, int n_kv_heads, int head_dim) {
 
 size_t xattn_decode_mx_workspace_bytes(int batch, int q_len, int n_q_heads, int n_kv_heads, int head_dim) {
     if (check_decode_shape(batch, q_len, n_q_heads, n_kv_heads, head_dim) != XATTN_OK) return 0;
+    if (n_kv_heads > kMxMaxHeads) {
+        fail(XATTN_EUNSUPPORTED, "xattn_decode_mx_workspace_bytes: %d KV heads: more than %d", n_kv_heads, kMxMaxHeads);
+        return 0;
+    }
     return decode_layout(batch, q_len, n_q_heads, mx_cut(q_len, n_q_heads, n_kv_heads).pieces).total;
 }
 
@@ -65,6 +70,7 @@ int xattn_decode_mx(const void* q, const void* const* k_ptrs, const void* const*
         return fail(XATTN_EINVAL, "%s: q, k_ptrs, v_ptrs, kv_lens and out must not be NULL", who);
     const int st = check_decode_shape(batch, q_len, n_q_heads, n_kv_heads, head_dim);
     if (st != XATTN_OK) return st;
+    if (n_kv_heads > kMxMaxHeads) return fail(XATTN_EUNSUPPORTED, "%s: %d KV heads: more than %d", who, n_kv_heads, kMxMaxHeads);
     const float scale_log2 = (float)((double)scale * 1.4426950408889634074);
     if (!std::isfinite(scale) || !std::isfinite(scale_log2)) return fail(XATTN_EINVAL, "%s: scale, or scale * log2 e, is not finite", who);
     if (misaligned(q, 16) || misaligned(out, 16)) return fail(XATTN_EINVAL, "%s: q and out must be 16-byte aligned", who);

@@ -23,7 +23,7 @@ def decode(q=A, k=A, v=A, lens=A, batch=2, q_len=1, hq=8, hkv=2, d=128, scale=0.
     (EINVAL, dict(batch=0)), (EINVAL, dict(q_len=0)), (EINVAL, dict(hq=0)), (EINVAL, dict(hkv=-2)), (EINVAL, dict(d=0)), (EINVAL, dict(scale=float("nan"))),
     (EINVAL, dict(scale=float("inf"))), (EINVAL, dict(scale=3e38)), (EINVAL, dict(scale=-3e38)), (EINVAL, dict(q=A + 8)), (EINVAL, dict(out=A + 2)),
     (EUNSUPPORTED, dict(batch=4097)), (EUNSUPPORTED, dict(q_len=17)), (EUNSUPPORTED, dict(hq=9)), (EUNSUPPORTED, dict(d=64)),
-    (EUNSUPPORTED, dict(q_len=16, hq=40, hkv=8))], ids=str)
+    (EUNSUPPORTED, dict(q_len=16, hq=40, hkv=8)), (EUNSUPPORTED, dict(hq=2048, hkv=1025)), (EUNSUPPORTED, dict(hq=1025, hkv=1025))], ids=str)
 def test_decode(status, change):
     refused(status, decode, **change)
 
@@ -84,7 +84,7 @@ def test_workspace_sizes():
     for batch, q_len, hq, hkv, pieces in ((64, 1, 32, 8, 32), (1, 4, 8, 2, 128), (3, 16, 4, 1, 128), (3, 1, 64, 64, 8), (5, 1, 5, 5, 48)):
         slots, rows = pieces + batch, q_len * hq
         assert xa.xattn_decode_mx_workspace_bytes(batch, q_len, hq, hkv) == up(batch * 8) + up(slots * rows * 8) + up(slots * rows * 512)
-    for args in ((0, 1, 8, 8), (1, 1, 8, 3), (1, 17, 8, 8), (4097, 1, 8, 8)):
+    for args in ((0, 1, 8, 8), (1, 1, 8, 3), (1, 17, 8, 8), (4097, 1, 8, 8), (1, 1, 1025, 1025)):
         with pytest.raises(xa.XattnError):
             xa.xattn_decode_mx_workspace_bytes(*args)
     for batch, q_len, vocab in ((1, 1, 1), (1, 5, 131072), (64, 5, 131072), (4096, 16, 40), (4096, 16, 2 ** 24)):
