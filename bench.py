@@ -44,7 +44,7 @@ sys.path.insert(0, os.path.join(ROOT, "tests"))
 HBM_PEAK_GBS = 8000.0
 MFMA_BF16_PEAK_TFLOPS = 2500.0
 TRAFFIC_JSON = os.path.join(ROOT, "profiles", "traffic.json")
-KERNEL_SOURCES = ["xattn_kernels.hip", "xattn_mla.hip", "xattn_device.h", "xattn_plan.h", "xattn_kernels.h"]
+KERNEL_SOURCES = ["xattn_kernels.hip", "xattn_mla.hip", "xattn_device.h", "xattn_matrix.h", "xattn_plan.h", "xattn_kernels.h"]
 
 
 def log(*a):
