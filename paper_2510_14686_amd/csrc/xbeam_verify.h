@@ -10,6 +10,7 @@ namespace xattn {
 constexpr int kVerifyThreads = 256;
 constexpr int kVerifyStep = 8 * kVerifyThreads;      // logits that a workgroup takes at a time
 constexpr int kVerifyMostParts = 64;                 // of a row: a wave puts them together, a lane each
+constexpr int kVerifySums = 5;                       // that a row's parts give
 
 struct VerifyParams {
     const void* target;              // [batch * q_len, >= vocab], rows target_stride values apart
@@ -27,7 +28,7 @@ struct VerifyParams {
     // workspace
     float2* stats;                   // [rows, parts]: reference, sum (greedy: and the best token's key)
     uint64_t* best;                  // [target rows, parts], greedy
-    double* sums;                    // [3, batch, cut.parts]: of the row's weights, of the draft's, of what is left
+    double* sums;                    // [kVerifySums, batch, cut.parts]: see verify_weigh_kernel
     void* decisions;                 // [batch]
 };
 
@@ -57,7 +58,7 @@ inline VerifyLayout verify_layout(int batch, int q_len, int vocab, bool with_dra
     w.pick = verify_cut(batch, vocab, kVerifyPickers);
     w.best_off = up((size_t)rows * w.read.parts * 8);
     w.sums_off = w.best_off + up((size_t)batch * q_len * w.read.parts * 8);
-    w.decisions_off = w.sums_off + up((size_t)3 * batch * w.pick.parts * 8);
+    w.decisions_off = w.sums_off + up((size_t)kVerifySums * batch * w.pick.parts * 8);
     w.total = w.decisions_off + up((size_t)batch * 64);
     return w;
 }

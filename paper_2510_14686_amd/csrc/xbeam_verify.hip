@@ -7,8 +7,7 @@
 // Steps, a kernel each:
 //   read     every row once, in parts: a reference and the sum of exponentials, in 32 bits
 //   decide   which drafts stand; the end of it with XBEAM_GREEDY
-//   weigh    the sums of p and q of the row that the new token comes from, part by part, in 64 bits
-//   rest     the sums of max(0, p - q), part by part (with a draft's probabilities only)
+//   weigh    the sums of p, q and max(0, p - q) of the row that the new token comes from, part by part, in 64 bits
 //   pick     the part that the random number falls into, and the token in it
 // 64 bits because the borders between 100000 tokens lie 10^-5 apart on average and closer where it matters: with sums in 32 bits one token in
 // a hundred would be another one's neighbour.  The row's probabilities are worked out anew in every pass: to keep them would be 8 bytes per logit.
@@ -31,6 +30,7 @@ constexpr int kWaves = kVerifyThreads / 64;
 // What the first pass says about a sequence.
 struct Decision {
     double top, draft_top;           // references of p's and q's exponents: the rows' maxima times scale * log2 e
+    double ratio;                    // with kRest: of the sums of p's and q's weights, from 32 bits
     int row;                         // token t that the new one is drawn at, or -1: no probabilities there
     int accepted;
     int mode;                        // kPlain, kRest, kWithout
@@ -213,7 +213,7 @@ __device__ __forceinline__ double logit_at(const void* rows, int64_t stride, int
 constexpr int kDecideWaves = 8;
 template <typename T, bool kGreedy>
 __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(VerifyParams prm, VerifyCut cut) {
-    __shared__ double lses[16], tops[16], draft_tops[16], lps[16];
+    __shared__ double lses[16], tops[16], draft_tops[16], ratios[16], lps[16];
     __shared__ int stands[16], tokens[16];
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), b = blockIdx.x, n = drafts_of(prm, b);
     const double c = (double)exponent_scale(prm.scale), dc = (double)exponent_scale(prm.draft_scale);
@@ -233,7 +233,7 @@ __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(Verify
         const double draft_at = is_token && with_draft ? logit_at<T>(prm.draft, prm.draft_stride, draft_row, x) : 0.0;
         const RowSum p = row_sum(mine);
         const double lp = at * c - p.log2_sum;
-        double draft_top = 0.0;
+        double draft_top = 0.0, ratio = 0.0;
         int best = -1;
         bool fine = false;
         if constexpr (kGreedy) {
@@ -251,6 +251,7 @@ __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(Verify
                 const RowSum q = row_sum(drafts);
                 draft_top = q.log2_sum - q.log2_sum == 0.0 ? q.top : __builtin_nan("");
                 lq = draft_at * dc - q.log2_sum;
+                ratio = exp2_d((p.log2_sum - p.top) - (q.log2_sum - q.top));
             }
             // u q < p, where the row has probabilities: NaN and infinities are neither
             fine = is_token && draft_top == draft_top && (double)prm.uniforms[row] * exp2_d(lq) < (lp == lp ? exp2_d(lp) : 0.0);
@@ -259,6 +260,7 @@ __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(Verify
             lses[t] = p.log2_sum;
             tops[t] = p.top;
             draft_tops[t] = draft_top;
+            ratios[t] = ratio;
             lps[t] = lp;
             stands[t] = fine;
             tokens[t] = kGreedy && !fine ? best : x;
@@ -271,6 +273,7 @@ __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(Verify
     const int at = d.accepted;
     d.top = tops[at];
     d.draft_top = draft_tops[at];
+    d.ratio = ratios[at];
     d.row = lses[at] - lses[at] == 0.0 ? at : -1;
     d.mode = kGreedy || at == n || !(d.draft_top == d.draft_top) ? kPlain : prm.draft ? kRest : kWithout;
     d.without = d.mode == kWithout && tokens[at] < prm.vocab ? tokens[at] : -1;
@@ -313,112 +316,107 @@ __device__ __forceinline__ void weights(const float (&x)[8], double c, double to
     for (int j = 0; j < 8; ++j) w[j] = exp2_d(__builtin_fma((double)x[j], c, -top));
 }
 
-__device__ __forceinline__ double block_sum_d(double x, int tid, double* space) {
-    x = wave_sum_d(x);
-    if ((tid & 63) == 0) space[tid >> 6] = x;
-    __syncthreads();
-    double all = space[0];
-    for (int w = 1; w < kWaves; ++w) all += space[w];
-    return all;
-}
+// With P and Q for the weights of p and q as they come and r for the ratio of their sums, max(0, p - q) is max(0, P - r Q) but for a factor.  Its sum
+// needs r first, yet the row is read once: the first pass says r0, off by 2^-21.6 of r at most in 1400 rows of 5000 to 131072 logits.  A token with
+// P - r0 Q further from 0 than |r - r0| Q stays on its side, and the sum over those above is, exactly,
+//     A - (r - r0) B      A = sum (P - r0 Q), B = sum Q      over tokens with P > r0 Q
+// The others change it by |r - r0| Q each at most: the fifth sum is of Q over all within kNear r0 Q, and where that leaves more than kMayMiss of the sum open, or
+// r is further off than kNear, pick sums anew with r, alone.  That happens where p and q are nearly the same, and, logits of 16 bits lying on a grid,
+// where one of its steps meets r: about one row in 4000 (bf16) or 500 (fp16), and costs 60 us at 131072 logits.  (A pass of its own with r: verify_batch 64.7 -> 57.9 us,
+// verify_one 20.6 -> 17.9.)
+constexpr double kNear = 0x1p-20, kMayMiss = 0x1p-30;
 
 // grid.x = parts, grid.y = sequences.
 template <typename T>
 __global__ __launch_bounds__(kVerifyThreads) void verify_weigh_kernel(VerifyParams prm, VerifyCut cut) {
-    __shared__ double space[2][kWaves];
+    __shared__ double space[kVerifySums][kWaves];
     const int tid = threadIdx.x, part = blockIdx.x, b = blockIdx.y;
     const Decision d = static_cast<const Decision*>(prm.decisions)[b];
     if (d.row < 0) return;
     const Source<T> s = source_of<T>(prm, b, d);
     const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
-    double sum = 0.0, draft_sum = 0.0;
+    double sums[kVerifySums] = {0.0, 0.0, 0.0, 0.0, 0.0};      // P, Q, A, B, near
+    const double near = kNear * d.ratio;
     for (int i = first + 8 * tid; i < end; i += kVerifyStep) {
         float x[8], y[8];
-        double w[8];
+        double w[8], v[8];
         load_logits(s.p + i, end - i, x);
         if (s.q) load_logits(s.q + i, end - i, y);
         weights(x, s.c, d.top, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum += i + j == d.without ? 0.0 : w[j];
+        for (int j = 0; j < 8; ++j) sums[0] += i + j == d.without ? 0.0 : w[j];
         if (s.q) {
-            weights(y, s.dc, d.draft_top, w);
+            weights(y, s.dc, d.draft_top, v);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) draft_sum += w[j];
+            for (int j = 0; j < 8; ++j) {
+                const double left = __builtin_fma(-d.ratio, v[j], w[j]);
+                sums[1] += v[j];
+                sums[2] += fmax(left, 0.0);
+                sums[3] += left > 0.0 ? v[j] : 0.0;
+                sums[4] += fabs(left) <= near * v[j] ? v[j] : 0.0;
+            }
         }
     }
-    sum = block_sum_d(sum, tid, space[0]);
-    draft_sum = block_sum_d(draft_sum, tid, space[1]);
-    if (tid == 0) {
-        prm.sums[(int64_t)b * cut.parts + part] = sum;
-        prm.sums[((int64_t)prm.batch + b) * cut.parts + part] = draft_sum;
+    const int n = s.q ? kVerifySums : 1;
+    for (int k = 0; k < n; ++k) {
+        const double sum = wave_sum_d(sums[k]);
+        if ((tid & 63) == 0) space[k][tid >> 6] = sum;
     }
+    __syncthreads();
+    if (tid >= n) return;
+    double all = space[tid][0];
+    for (int w = 1; w < kWaves; ++w) all += space[tid][w];
+    prm.sums[((int64_t)tid * prm.batch + b) * cut.parts + part] = all;
 }
 
-// ---------------------------------------------------------------------------------- rest and pick
-// What 1 / sum p and 1 / sum q are, from the parts' sums: by every wave.
-struct Norms {
-    double p, q;
-};
-__device__ __forceinline__ Norms norms_of(const VerifyParams& prm, const VerifyCut& cut, int b, int lane) {
-    const double p = wave_sum_d(lane < cut.parts ? prm.sums[(int64_t)b * cut.parts + lane] : 0.0);
-    const double q = wave_sum_d(lane < cut.parts ? prm.sums[((int64_t)prm.batch + b) * cut.parts + lane] : 0.0);
-    return Norms{1.0 / p, 1.0 / q};
-}
-// max(0, p - q) of eight tokens.
-template <typename T>
-__device__ __forceinline__ void rest_of(const Source<T>& s, const Decision& d, const Norms& norm, int i, int end, double (&w)[8]) {
-    float x[8], y[8];
-    double v[8];
-    load_logits(s.p + i, end - i, x);
-    load_logits(s.q + i, end - i, y);
-    weights(x, s.c, d.top, w);
-    weights(y, s.dc, d.draft_top, v);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) w[j] = fmax(w[j] * norm.p - v[j] * norm.q, 0.0);
-}
-
-template <typename T>
-__global__ __launch_bounds__(kVerifyThreads) void verify_rest_kernel(VerifyParams prm, VerifyCut cut) {
-    __shared__ double space[kWaves];
-    const int tid = threadIdx.x, part = blockIdx.x, b = blockIdx.y;
-    const Decision d = static_cast<const Decision*>(prm.decisions)[b];
-    if (d.row < 0 || d.mode != kRest) return;
-    const Source<T> s = source_of<T>(prm, b, d);
-    const Norms norm = norms_of(prm, cut, b, tid & 63);
-    const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
-    double sum = 0.0;
-    for (int i = first + 8 * tid; i < end; i += kVerifyStep) {
-        double w[8];
-        rest_of(s, d, norm, i, end, w);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) sum += w[j];
-    }
-    sum = block_sum_d(sum, tid, space);
-    if (tid == 0) prm.sums[((int64_t)2 * prm.batch + b) * cut.parts + part] = sum;
-}
-
+// ---------------------------------------------------------------------------------- pick
 // A workgroup per sequence: the part that holds the random number's share of the sum, then step by step the logits of that part.  Bound by the
 // fetching of its own instructions, each of which it needs once: four logits per thread (of 512) instead of eight.
 constexpr int kPickThreads = 512, kPickWaves = kPickThreads / 64, kPickLogits = kVerifyStep / kPickThreads;
 template <typename T>
 __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams prm, VerifyCut cut) {
     __shared__ double totals[kPickWaves];
+    __shared__ double again[kVerifyMostParts];
     __shared__ int tops[kPickWaves], heres[kPickWaves];      // a wave's last token with a weight, and the first beyond the goal
     const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), b = blockIdx.x;
     const double u = (double)prm.uniforms[(int64_t)b * prm.q_len + prm.q_len - 1];
-    double part_sums[3];      // all that may be needed, in one round trip
+    double sums[kVerifySums];      // all that may be needed, in one round trip
 #pragma unroll
-    for (int k = 0; k < 3; ++k) part_sums[k] = lane < cut.parts && (k < 2 || prm.draft) ? prm.sums[((int64_t)k * prm.batch + b) * cut.parts + lane] : 0.0;
+    for (int k = 0; k < kVerifySums; ++k) sums[k] = lane < cut.parts && (k == 0 || prm.draft) ? prm.sums[((int64_t)k * prm.batch + b) * cut.parts + lane] : 0.0;
     const Decision d = static_cast<const Decision*>(prm.decisions)[b];
     constexpr int kNone = 0x7fffffff;
     int last = -1;
     const int64_t out = (int64_t)b * prm.q_len + d.accepted;
-    const double upto_p = wave_scan_d(part_sums[0]), all_p = lane_d(upto_p, 63);
-    const Norms norm = {1.0 / all_p, 1.0 / wave_sum_d(part_sums[1])};
-    const double upto_rest = wave_scan_d(part_sums[2]), all_rest = lane_d(upto_rest, 63);
+    const double upto_p = wave_scan_d(sums[0]), all_p = lane_d(upto_p, 63), ratio = all_p / wave_sum_d(sums[1]);
+    const Source<T> s = source_of<T>(prm, b, d);
+    const bool drafted = d.row >= 0 && d.mode == kRest;
+    const double less = ratio - d.ratio;
+    double left = fmax(__builtin_fma(-less, sums[3], sums[2]), 0.0), upto_left = wave_scan_d(left), all_left = lane_d(upto_left, 63);
+    if (uniform(drafted && !(fabs(less) <= 0.999 * kNear * d.ratio && fabs(less) * wave_sum_d(sums[4]) <= kMayMiss * all_left))) {
+        for (int part = wave; part < cut.parts; part += kPickWaves) {
+            const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
+            double sum = 0.0;
+            for (int i = first + 8 * lane; i < end; i += 8 * 64) {
+                float x[8], y[8];
+                double w[8], v[8];
+                load_logits(s.p + i, end - i, x);
+                load_logits(s.q + i, end - i, y);
+                weights(x, s.c, d.top, w);
+                weights(y, s.dc, d.draft_top, v);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) sum += fmax(__builtin_fma(-ratio, v[j], w[j]), 0.0);
+            }
+            sum = wave_sum_d(sum);
+            if (lane == 0) again[part] = sum;
+        }
+        __syncthreads();
+        left = lane < cut.parts ? again[lane] : 0.0;
+        upto_left = wave_scan_d(left);
+        all_left = lane_d(upto_left, 63);
+    }
     // p nowhere above q: nothing could have fallen but by rounding
-    const bool rest = d.row >= 0 && d.mode == kRest && all_rest > 0.0;
-    const double all = rest ? all_rest : all_p, upto = rest ? upto_rest : upto_p, mine = rest ? part_sums[2] : part_sums[0];
+    const bool rest = drafted && all_left > 0.0;
+    const double all = rest ? all_left : all_p, upto = rest ? upto_left : upto_p, mine = rest ? left : sums[0];
     if (d.row < 0 || !(all > 0.0) || !(all < __builtin_inf())) {
         if (tid == 0) {
             // without a token that has all of p, it comes back: rounding alone let it fall
@@ -428,7 +426,6 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams 
         }
         return;
     }
-    const Source<T> s = source_of<T>(prm, b, d);
     auto finish = [&](int token, double logit) {
         prm.tokens[out] = token;
         if (prm.token_lp) {
@@ -457,7 +454,7 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams 
 #pragma unroll
         for (int j = 0; j < kPickLogits; ++j) {
             w[j] = i + j == d.without ? 0.0 : exp2_d(__builtin_fma((double)x[j], s.c, -d.top));
-            if (rest) w[j] = fmax(w[j] * norm.p - exp2_d(__builtin_fma((double)y[j], s.dc, -d.draft_top)) * norm.q, 0.0);
+            if (rest) w[j] = fmax(__builtin_fma(-ratio, exp2_d(__builtin_fma((double)y[j], s.dc, -d.draft_top)), w[j]), 0.0);
             sum += w[j];
             top = w[j] > 0.0 ? i + j : top;
         }
@@ -510,7 +507,6 @@ hipError_t launch_type(const VerifyParams& prm, const VerifyLayout& w, hipStream
     const dim3 grid((unsigned)w.pick.parts, (unsigned)prm.batch);
     hipError_t e = launch_first<T, false>(prm, w, stream);
     if (e == hipSuccess) e = launch(verify_weigh_kernel<T>, grid, kVerifyThreads, stream, prm, w.pick);
-    if (e == hipSuccess && prm.draft) e = launch(verify_rest_kernel<T>, grid, kVerifyThreads, stream, prm, w.pick);
     return e != hipSuccess ? e : launch(verify_pick_kernel<T>, dim3((unsigned)prm.batch), kPickThreads, stream, prm, w.pick);
 }
 

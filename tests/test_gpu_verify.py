@@ -5,6 +5,7 @@ no random number of these inputs lies that near to a border.  token_lp: 2^-20 fo
 """
 import math
 
+import numpy as np
 import pytest
 import torch
 
@@ -19,9 +20,12 @@ def reference(target, draft, scale, draft_scale, draft_tokens, counts, uniforms,
     batch, q_len, vocab = target.shape
     tokens, accepted, lps = [], [], []
 
-    def probabilities(x, s):
+    def probabilities(x, s):      # step by step: torch.softmax of doubles on the GPU is off by 2e-6 of them
         x = x.double() * s
-        return torch.softmax(x, 0) if bool((x < math.inf).all()) and bool((x > -math.inf).any()) else None
+        if not bool((x < math.inf).all()) or not bool((x > -math.inf).any()):
+            return None
+        e = torch.exp(x - x.max())
+        return e / e.sum()
 
     for b in range(batch):
         n = min(max(counts[b], 0), q_len - 1)
@@ -243,6 +247,28 @@ def test_a_draft_of_the_targets_own_probabilities_stands():
     c.uniforms.fill_(1.0 - 2.0 ** -10)
     c.call()
     assert c.check() == [5] * 50
+
+
+@pytest.mark.parametrize("by", [0.0, 1e-6, 1e-5, 1e-4, 1e-3, 1e-2])
+@pytest.mark.parametrize("tokens", [8, 400, 20000])
+def test_probabilities_that_are_nearly_equal(tokens, by):
+    """A draft row off the target's by `by` at so many tokens: what is left over is as small, below 2^-30 of p where doubles would leave open which
+    of 20000 tokens it is, so the definition is computed with 64 bits of significand.  The drafts, which are no tokens, fall."""
+    c = Case(48, 3, 20000, "fp32", seed=tokens + int(1 / by if by else 0))
+    g = torch.Generator(device="cuda")
+    g.manual_seed(tokens)
+    at = torch.randperm(20000, generator=g, device="cuda")[:tokens]
+    c.draft.copy_(c.target[:, :-1])
+    c.draft[..., at] += by * torch.randn((48, 2, tokens), generator=g, device="cuda")
+    c.draft_tokens.fill_(-1)
+    c.call()
+    assert c.accepted.tolist() == [0] * 48
+    target, draft, u = (x.cpu().numpy().astype(np.longdouble) for x in (c.target[:, 0], c.draft[:, 0], c.uniforms[:, -1]))
+    for b in range(48):
+        p, q = (np.exp(x[b] - x[b].max()) for x in (target, draft))
+        w = np.maximum(p / p.sum() - q / q.sum(), 0)
+        sums = np.cumsum(w if w.sum() > 0 else p)
+        assert int(c.tokens[b, 0]) == int(np.argmax(sums > u[b] * sums[-1])), b
 
 
 @pytest.mark.parametrize("far", [3e4, -3e4])
