@@ -2,8 +2,17 @@
 //
 //   s_j = scale <q, k_j>;  out = sum_j softmax(s)_j v_j;  lse = ln sum_j exp(s_j)      with k_j = 2^e code, v_j likewise, per block of 32 values
 //
-// The stream of keys is cut as xattn_decode's is, in whole tiles: a workgroup takes a piece of it for one KV head, its eight waves a
+// The stream of keys is cut as xattn_decode's is, in whole tiles: a workgroup takes a piece of it for one KV head, its waves (mx_cut) a
 // run of tiles each; a sequence that the waves cut among themselves is put together in LDS, one that pieces cut by the merge kernel.
+//
+// Bound by HBM with many keys: 64 sequences of 512 to 4096, 32 / 8 heads, 35.2 us; 16 of 16384 to 32768, 64 / 8 heads, 76 us (5.9 TB/s); 128 of
+// 1028 to 8196, four tokens, 32 / 8 heads, 107 us (5.8 TB/s); with few by the dependent steps of two kernels, 9 to 10 us.  What the code owes to that:
+//  - Codes become bf16 by a conversion with the scale, exactly, two to an instruction, and enter bf16 matrix products.  The scaled products
+//    that take codes as they are would want q in 8 bits: in three parts of e4m3 their sums are off by 7e-5 of sum |q k|, these by 1e-7.
+//  - Codes lie as the products' lanes hold them, so every load is 16 bytes a lane of one run of 1 KiB and nothing passes through LDS.
+//  - A wave holds one tile, and where its K (V) has been used the next one's loads go out into its place; twelve waves a compute unit
+//    wait for theirs in turn.  (Two tiles in registers and eight waves: 38.0 us in place of 35.5, 79.6 of 76.)
+//  - Softmax weights enter the value product as two bf16, 16 bits.  With one, 8 bits, a call takes 2 to 3 % less, with 64 rows to a KV head 12 %.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -22,9 +31,12 @@ struct TileUnit {
     static __device__ __forceinline__ int stream(int raw, int seg_cost) { return raw > 0 ? mx_positions(raw) + seg_cost : 0; }
 };
 
+// How far, in powers of two, a score may exceed its row's reference before that moves.  (0: 64 sequences of 512 to 4096 35.2 -> 37.1 us, 32 rows to a KV
+// head 45.9 -> 47.2; sums stay within 2^8 times a row's keys.)
 constexpr float kSlack = 8.0f;
 
-// Fixed work of a (piece, sequence) segment, in positions.
+// Fixed work of a (piece, sequence) segment, in positions: a tile's.  (None / one / two / four tiles' worth: 64 sequences of 512 to 4096 37.2 / 35.2 / 36.3 /
+// 37.0 us; 222 of 16 to 60000 66.3 / 65.2 / 64.5 / 67.1; 256 of up to 400 21.9 / 21.3 / 20.5 / 22.7.)
 constexpr int kMxSegCost = kMxPositions;
 
 // Lane (kb, n) = (lane / 16, lane % 16) of a tile: K's block kb of tokens 16 s + n; V's values 8 n .. 8 n + 7 of tokens 16 s + 4 kb + r.
@@ -87,7 +99,6 @@ __device__ __forceinline__ void mx_tile(MatrixState (&st)[kTiles], const MxTile&
         float mx = kNegInf;
 #pragma unroll
         for (int i = 0; i < 4; ++i) mx = fmaxf(mx, fmaxf(fmaxf(s[t][i][0], s[t][i][1]), fmaxf(s[t][i][2], s[t][i][3])));
-        // The reference moves when a score exceeds it by 2^8 or more: no weight exceeds that, and few tiles move it.
         if (__builtin_amdgcn_ballot_w64(mx * scale_log2 > st[t].m + kSlack) != 0) {
             mx = kb_max(mx) * scale_log2;
             const bool moves = mx > st[t].m;
@@ -206,7 +217,6 @@ __device__ __forceinline__ void mx_run(MatrixState (&st)[kTiles], MxCtx<kTiles>&
     }
     const int64_t step = (int64_t)prm.n_kv_heads * kMxTileBytes;
     const int first = c.seg.j0 / kMxPositions, n_tiles = c.seg.j1 / kMxPositions - first;
-    // Two tiles in registers, and where one's codes have been used the loads of the tile after the next go out into their place.
     const float scale_log2 = prm.scale_log2 == 0.0f ? 1.0f : fabsf(prm.scale_log2);
     auto k_at = [&](int i) { return c.kp + i * step; };
     auto v_at = [&](int i) { return c.vp + i * step; };
