@@ -94,12 +94,13 @@ size_t xbeam_logprobs_workspace_bytes(int rows, int vocab, int top_k);
  * tokens       DEVICE int32 [batch, q_len]: the drafts that stand, the new token, then -1
  * n_accepted   DEVICE int32 [batch]: drafts that stand; a sequence keeps kv_len - (q_len - 1 - n_accepted) rows of its cache
  * token_lp     DEVICE fp32 [batch, q_len] or NULL: ln p of every token given, 0 behind them
+ * Outputs do not overlap the inputs or each other.
  * Logits of -inf are forbidden tokens.  A target row with +inf or NaN, or of nothing but -inf, has no probabilities: its draft falls, and the new
  * token is -1 (token_lp NaN).  At a draft row without probabilities the draft falls and w = p.  Where rounding alone let a draft fall, p being
  * nowhere above q, w = p.
- * Numerics: whether a draft stands is decided with sums in 32 bits (p and q off by 2^-20 of them at most); the new token's sums are kept in 64
- * bits, since the borders between tokens lie closer together than 32 bits tell (that of w = max(0, p_t - q_t) is off by 2^-30 of it at most).  Every call
- * with the same inputs gives the same bits.
+ * Numerics: whether a draft stands is decided with sums in 32 bits: p and q are off by 2^-20 of them at most, and 2^-25 for every power of two
+ * below 1.  The new token's sums are kept in 64 bits, since the borders between tokens lie closer together than 32 bits tell; that of
+ * w = max(0, p_t - q_t) is off by 2^-30 of it at most.  Every call with the same inputs gives the same bits.
  * batch 1..4096, q_len 1..16, vocab 1..2^24.  Asynchronous on `stream`, which it may be captured on; takes the stream's workspace
  * (xattn_set_workspace; xbeam_verify_workspace_bytes: what one call needs of it), with the rules that xattn_decode states.
  */

@@ -156,6 +156,13 @@ def test_batches(batch, vocab):
         assert set(accepted) == {0, 1, 2, 3}
 
 
+@pytest.mark.parametrize("drafts", ["logits", "certain"])
+def test_the_largest_vocabulary(drafts):
+    c = Case(2, 2, 1 << 24, "bf16", drafts, seed=8, sd=1.5)
+    c.call()
+    c.check()
+
+
 def test_most_rows():
     """A batch of 4096 with 16 rows each: their number passes 65535."""
     c = Case(4096, 16, 40, "bf16", seed=1, near=0.1)
@@ -249,6 +256,17 @@ def test_a_draft_of_the_targets_own_probabilities_stands():
     assert c.check() == [5] * 50
 
 
+def check_what_is_left(c):
+    """The first draft falls; the new token, by the definition with 64 bits of significand."""
+    assert c.accepted.tolist() == [0] * c.batch
+    target, draft, u = (x.cpu().numpy().astype(np.longdouble) for x in (c.target[:, 0], c.draft[:, 0], c.uniforms[:, -1]))
+    for b in range(c.batch):
+        p, q = (np.exp(x[b] - x[b].max()) for x in (target, draft))
+        w = np.maximum(p / p.sum() - q / q.sum(), 0)
+        sums = np.cumsum(w if w.sum() > 0 else p)
+        assert int(c.tokens[b, 0]) == int(np.argmax(sums > u[b] * sums[-1])), b
+
+
 @pytest.mark.parametrize("by", [0.0, 1e-6, 1e-5, 1e-4, 1e-3, 1e-2])
 @pytest.mark.parametrize("tokens", [8, 400, 20000])
 def test_probabilities_that_are_nearly_equal(tokens, by):
@@ -262,13 +280,25 @@ def test_probabilities_that_are_nearly_equal(tokens, by):
     c.draft[..., at] += by * torch.randn((48, 2, tokens), generator=g, device="cuda")
     c.draft_tokens.fill_(-1)
     c.call()
-    assert c.accepted.tolist() == [0] * 48
-    target, draft, u = (x.cpu().numpy().astype(np.longdouble) for x in (c.target[:, 0], c.draft[:, 0], c.uniforms[:, -1]))
-    for b in range(48):
-        p, q = (np.exp(x[b] - x[b].max()) for x in (target, draft))
-        w = np.maximum(p / p.sum() - q / q.sum(), 0)
-        sums = np.cumsum(w if w.sum() > 0 else p)
-        assert int(c.tokens[b, 0]) == int(np.argmax(sums > u[b] * sums[-1])), b
+    check_what_is_left(c)
+
+
+@pytest.mark.parametrize("tokens", [2, 40, 5000])
+@pytest.mark.parametrize("vocab", [12000, 131072])
+def test_probabilities_that_are_nearly_equal_but_for_some_tokens(vocab, tokens):
+    """Pairs of tokens one of which a draft row gives what the other has in the target's: the ratio of the sums is that of all other tokens."""
+    c = Case(48, 3, vocab, "fp32", seed=tokens)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(tokens)
+    at = torch.randperm(vocab, generator=g, device="cuda")[:2 * tokens]
+    c.draft.copy_(c.target[:, :-1])
+    x = c.target[:, :-1][..., at]
+    more = torch.log(x.exp().unflatten(-1, (2, tokens)).sum(2))
+    c.draft[..., at[:tokens]] = more + math.log(0.9)
+    c.draft[..., at[tokens:]] = more + math.log(0.1)
+    c.draft_tokens.fill_(-1)
+    c.call()
+    check_what_is_left(c)
 
 
 @pytest.mark.parametrize("far", [3e4, -3e4])
