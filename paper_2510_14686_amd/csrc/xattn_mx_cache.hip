@@ -3,8 +3,8 @@
 //   append  (x, y) -> (x cos a - y sin a, y cos a + x sin a) as in xattn_rope.hip; q rounded to bf16, k and v to codes with a scale per 32 values
 //   read    code * scale, exact in bf16
 //
-// A prompt's append is bound by HBM and, beside it, the arithmetic of codes: two prompts of 4096 to 8191 tokens, 32 / 8 heads, three axes, 262 MB in
-// 66 us, 4.0 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
+// A prompt's append is bound by HBM and, beside it, the arithmetic of codes: two prompts of 4096 to 8191 tokens, 32 / 8 heads, three axes, 273 MB in
+// 66 us, 4.1 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
 // rounded to bf16, in 32.  V, which is not turned, takes 32 bits with the same codes (94.6 -> 79 us for the append and the reading of it).  One row to a workgroup / two /
 // four: 89 / 79 / 83 us; the rule is xattn_rope.hip's.  A step of few tokens is bound by the host's call, its kernel takes 5 us.
 #include <hip/hip_runtime.h>
