@@ -6,7 +6,7 @@
 // A prompt's append is bound by HBM and, beside it, the arithmetic of codes: two prompts of 4096 to 8191 tokens, 32 / 8 heads, three axes, 273 MB in
 // 66 us, 4.1 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
 // rounded to bf16, in 32.  V, which is not turned, takes 32 bits with the same codes (94.6 -> 79 us for the append and the reading of it).  One row to a workgroup / two /
-// four: 89 / 79 / 83 us; the rule is xattn_rope.hip's.  A step of few tokens is bound by the host's call, its kernel takes 5 us.
+// four: 89 / 79 / 83 us.  A step of few tokens is bound by the host's call, its kernel takes 5 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -334,6 +334,14 @@ __global__ __launch_bounds__(256) void read_mx_kernel(ReadMxParams prm) {
     }
 }
 
+// Rows per workgroup.  Fewer rows, more workgroups whose waits pass at once; more rows, fewer threads without work.  Of 1 / 2 / 4 rows each, in us: 256 rows of 40 / 8 heads
+// 5.5 / 7.3 / 10.6, 1024 8.8 / 9.8 / 12.2, 2048 15.3 / 13.4 / 16.0, 8192 43.6 / 38.2 / 41.1; of 64 / 8 1024 10.8 / 11.6 / 14.7, 8192 63 / 60.6 / 64; of 8 / 2 1024
+// 5.6 / 5.8 / 5.4, 4096 12.7 / 10.1 / 8.5, 8192 22.8 / 18.0 / 15.2.
+int rows_per_workgroup(const RopeParams& prm) {
+    if (prm.total_q < 1536) return 1;
+    return (prm.n_q_heads + 2 * prm.n_kv_heads) * (kHeadDim / 16) > kRopeThreads / 2 ? 2 : 4;
+}
+
 }  // namespace
 
 hipError_t launch_rope_mx(const RopeParams& prm, hipStream_t stream) {
@@ -341,7 +349,7 @@ hipError_t launch_rope_mx(const RopeParams& prm, hipStream_t stream) {
         constexpr int kTokens = decltype(tokens)::value;
         return launch(rope_mx_kernel<kTokens>, dim3((unsigned)((prm.total_q + kTokens - 1) / kTokens)), kRopeThreads, stream, prm);
     };
-    switch (rope_rows_per_workgroup(prm.total_q, prm.n_q_heads, prm.n_kv_heads, prm.head_dim)) {
+    switch (rows_per_workgroup(prm)) {
         case 1: return with(std::integral_constant<int, 1>());
         case 2: return with(std::integral_constant<int, 2>());
         default: return with(std::integral_constant<int, 4>());
