@@ -5,8 +5,9 @@
 //
 // A prompt's append is bound by HBM and, beside it, the arithmetic of codes: two prompts of 4096 to 8191 tokens, 32 / 8 heads, three axes, 273 MB in
 // 66 us, 4.1 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
-// rounded to bf16, in 32.  V, which is not turned, takes 32 bits with the same codes (94.6 -> 79 us for the append and the reading of it).  One row to a workgroup / two /
-// four: 89 / 79 / 83 us.  A step of few tokens is bound by the host's call, its kernel takes 5 us.
+// rounded to bf16, in 32.  V, which is not turned, takes 32 bits with the same codes.  One row to a workgroup / two / four: 89 / 79 / 83 us for the append and the reading of it.
+// q, k and v are read and q is written past the caches: 8 prompts of 1024 tokens whose q, k and v a kernel before wrote 40.6 -> 28.6 us, with the xattn_prefill behind it 39.1 -> 32 (of
+// which it took its part); 64 of 256 81 -> 70, 256 of 16, 40 / 8 heads, 25 -> 21; steps of few tokens level.  A step's kernel takes 5 us, and the host's call binds it.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -105,6 +106,10 @@ __device__ __forceinline__ Encoded encode(u32x4_t x) {
     return Encoded{convert(f, __uint_as_float((uint32_t)(e + 127) << 23)), most < 0x7f80u ? e + 127 : kMxNanScale};
 }
 
+// Values that are read once, or that this kernel does not need again: past the caches, which keep what else is in them.
+__device__ __forceinline__ u32x4_t load_once(const uint16_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)); }
+__device__ __forceinline__ void store_past(u32x4_t x, uint16_t* p) { __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t*>(p)); }
+
 __device__ __forceinline__ void widen(u32x4_t x, double (&d)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -151,8 +156,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
         r.at1 = apart ? F + 8 * r.c : 16 * r.c + 8;
         r.at = (row * prm.n_q_heads + head) * kHeadDim;
         const uint16_t* const from = prm.q + row * prm.q_stride + head * kHeadDim;
-        r.x = *reinterpret_cast<const u32x4_t*>(from + r.at0);
-        r.y = *reinterpret_cast<const u32x4_t*>(from + r.at1);
+        r.x = load_once(from + r.at0);
+        r.y = load_once(from + r.at1);
         return r;
     };
     // k and v: 8 values of a head at a time, 16 lanes a head
@@ -172,7 +177,7 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
         r.second = 8 * r.m >= F;
         const int64_t row = token0 + r.tk < prm.total_q ? token0 + r.tk : prm.total_q - 1;
         const uint16_t* const from = (r.is_v ? prm.v + row * prm.v_stride : prm.k + row * prm.k_stride) + r.head * kHeadDim;
-        r.x = *reinterpret_cast<const u32x4_t*>(from + 8 * r.m);
+        r.x = load_once(from + 8 * r.m);
         r.other = r.x;
         if (!halves && !prm.pairs && !r.is_v && r.m < 2 * turned) r.other = *reinterpret_cast<const u32x4_t*>(from + (r.second ? 8 * r.m - F : 8 * r.m + F));
         return r;
@@ -235,8 +240,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
                 }
             }
         }
-        *reinterpret_cast<u32x4_t*>(prm.q_out + it.at + it.at0) = x;
-        *reinterpret_cast<u32x4_t*>(prm.q_out + it.at + it.at1) = y;
+        store_past(x, prm.q_out + it.at + it.at0);
+        store_past(y, prm.q_out + it.at + it.at1);
     }
 
     for (int item = tid; item < kv_all; item += kRopeThreads) {
@@ -278,8 +283,13 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
 
 // A wave takes four rows, 16 lanes a row, of four heads (grid.y): a row's sequence is looked for once for them, and rows that follow each other share
 // the lines of the cache.  (All heads in a workgroup: 500 rows of 40 heads 7.2 -> 10.6 us, large calls level.)  Bound by HBM: 28672 rows of 8
-// heads 33.5 us, 4.4 TB/s.
+// heads 24.5 us, 6.1 TB/s.
+// Results of 8 MiB and more go past the caches (kPast).  Written through them, they push out lines that others then have to write: that call 33.7 us, and 48 where a kernel before it
+// left the caches full, 32 so.  A following xattn_prefill of 128 tokens, which finds less there, takes most of that back: both 114 us and 115; 36.0 and 34.5 with 4096
+// rows, 206 and 211 with 65536, 20.0 and 21.4 with 512, which stay in the caches.
+constexpr int64_t kReadPast = (8 << 20) / (4 * kHeadDim);      // rows of heads, K's and V's
 constexpr int kReadRows = 16, kReadHeads = 4;
+template <bool kPast>
 __global__ __launch_bounds__(256) void read_mx_kernel(ReadMxParams prm) {
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), m = lane & 15;
     const int row0 = blockIdx.x * kReadRows + 4 * wave;
@@ -329,8 +339,15 @@ __global__ __launch_bounds__(256) void read_mx_kernel(ReadMxParams prm) {
 #pragma unroll
     for (int h = 0; h < kReadHeads; ++h) {
         if (head0 + h >= prm.n_kv_heads) break;
-        *reinterpret_cast<u32x4_t*>(prm.k_out + to + (head0 + h) * kHeadDim) = unpack(kc[h], ks[h]);
-        *reinterpret_cast<u32x4_t*>(prm.v_out + to + (head0 + h) * kHeadDim) = unpack(vc[h], vs[h]);
+        uint16_t* const k = prm.k_out + to + (head0 + h) * kHeadDim;
+        uint16_t* const v = prm.v_out + to + (head0 + h) * kHeadDim;
+        if constexpr (kPast) {
+            store_past(unpack(kc[h], ks[h]), k);
+            store_past(unpack(vc[h], vs[h]), v);
+        } else {
+            *reinterpret_cast<u32x4_t*>(k) = unpack(kc[h], ks[h]);
+            *reinterpret_cast<u32x4_t*>(v) = unpack(vc[h], vs[h]);
+        }
     }
 }
 
@@ -358,7 +375,8 @@ hipError_t launch_rope_mx(const RopeParams& prm, hipStream_t stream) {
 
 hipError_t launch_read_mx(const ReadMxParams& prm, hipStream_t stream) {
     const int rows = (prm.total_q + kReadRows - 1) / kReadRows, heads = (prm.n_kv_heads + kReadHeads - 1) / kReadHeads;
-    return launch(read_mx_kernel, dim3((unsigned)rows, (unsigned)heads), 256, stream, prm);
+    const dim3 grid((unsigned)rows, (unsigned)heads);
+    return (int64_t)prm.total_q * prm.n_kv_heads >= kReadPast ? launch(read_mx_kernel<true>, grid, 256, stream, prm) : launch(read_mx_kernel<false>, grid, 256, stream, prm);
 }
 
 }  // namespace xattn
