@@ -26,10 +26,10 @@ typedef uint32_t words_at_4 __attribute__((ext_vector_type(4), aligned(4)));
 template <typename T> struct Chunk {
     static constexpr int kCount = 16 / (int)sizeof(T);
     u32x4_t x;
-    __device__ __forceinline__ void load(const T* p) {
-        using words = typename std::conditional<sizeof(T) == 4, words_at_4, words_at_2>::type;
-        x = __builtin_nontemporal_load(reinterpret_cast<const words*>(p));
-    }
+    using words = typename std::conditional<sizeof(T) == 4, words_at_4, words_at_2>::type;
+    __device__ __forceinline__ void load(const T* p) { x = __builtin_nontemporal_load(reinterpret_cast<const words*>(p)); }
+    // Of a row that is read again.
+    __device__ __forceinline__ void load_kept(const T* p) { x = *reinterpret_cast<const words*>(p); }
     __device__ __forceinline__ float get(int i) const {
         if constexpr (sizeof(T) == 4) return __uint_as_float(x[i]);
         else if constexpr (std::is_same<T, Bf16>::value) return i & 1 ? bf16_hi(x[i >> 1]) : bf16_lo(x[i >> 1]);

@@ -43,14 +43,15 @@ constexpr int kPlain = 0, kRest = 1, kWithout = 2;
 static_assert(sizeof(Decision) <= 64, "verify_layout");
 
 // Eight logits from p on, as far as there are so many; the others -inf.
-template <typename T>
+template <bool kKeep = false, typename T>
 __device__ __forceinline__ void load_logits(const T* p, int left, float (&x)[8]) {
     if (left >= 8) {
         constexpr int kCount = Chunk<T>::kCount;
 #pragma unroll
         for (int c = 0; c < 8 / kCount; ++c) {
             Chunk<T> chunk;
-            chunk.load(p + c * kCount);
+            if constexpr (kKeep) chunk.load_kept(p + c * kCount);
+            else chunk.load(p + c * kCount);
 #pragma unroll
             for (int i = 0; i < kCount; ++i) x[c * kCount + i] = chunk.get(i);
         }
@@ -123,8 +124,11 @@ __device__ __forceinline__ int drafts_of(const VerifyParams& prm, int b) {
 }
 
 // ---------------------------------------------------------------------------------- read
-// grid.x = rows, those of the target, then those of the draft; grid.y = parts.
-template <typename T, bool kGreedy>
+// grid.x = rows, those of the target, then those of the draft; grid.y = parts.  Up to kKeepBytes of logits stay in the caches (kKeep) for the kernels
+// that read a row of them again: 48 sequences of four rows of 100003 in fp32 (77 MB) 29.8 -> 27.8 us, 64 of four of 128256 in bf16 (66 MB) 33.5 -> 32.6, 128 of seven of
+// 50000 (90 MB) 42.4 -> 42.1; but 48 of nine of 131072 (113 MB) 49.5 -> 50.0, 64 of them (151 MB) 56.5 -> 59.
+constexpr int64_t kKeepBytes = 96 << 20;
+template <typename T, bool kGreedy, bool kKeep>
 __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParams prm, VerifyCut cut) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, part = blockIdx.y;
     const int target_rows = prm.batch * prm.q_len, row = blockIdx.x;
@@ -142,7 +146,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
         constexpr int kCount = decltype(count)::value;
         float x[kCount][8];
 #pragma unroll
-        for (int k = 0; k < kCount; ++k) load_logits(p + i + k * kVerifyStep, end - i - k * kVerifyStep, x[k]);
+        for (int k = 0; k < kCount; ++k) load_logits<kKeep>(p + i + k * kVerifyStep, end - i - k * kVerifyStep, x[k]);
         float top = x[0][0];
 #pragma unroll
         for (int k = 0; k < kCount; ++k)
@@ -501,7 +505,10 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams 
 template <typename T, bool kGreedy>
 hipError_t launch_first(const VerifyParams& prm, const VerifyLayout& w, hipStream_t stream) {
     const long rows = (long)prm.batch * (prm.draft ? 2 * prm.q_len - 1 : prm.q_len);
-    const hipError_t e = launch(verify_read_kernel<T, kGreedy>, dim3((unsigned)rows, (unsigned)w.read.parts), kVerifyThreads, stream, prm, w.read);
+    const dim3 grid((unsigned)rows, (unsigned)w.read.parts);
+    hipError_t e;
+    if (!kGreedy && rows * prm.vocab * (int64_t)sizeof(T) <= kKeepBytes) e = launch(verify_read_kernel<T, kGreedy, !kGreedy>, grid, kVerifyThreads, stream, prm, w.read);
+    else e = launch(verify_read_kernel<T, kGreedy, false>, grid, kVerifyThreads, stream, prm, w.read);
     return e != hipSuccess ? e : launch(verify_decide_kernel<T, kGreedy>, dim3((unsigned)prm.batch), 64 * kDecideWaves, stream, prm, w.read);
 }
 template <typename T>
