@@ -4,7 +4,7 @@
 //   read    code * scale, exact in bf16
 //
 // A prompt's append is bound by HBM and, beside it, the arithmetic of codes: two prompts of 4096 to 8191 tokens, 32 / 8 heads, three axes, 273 MB in
-// 66 us, 4.1 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
+// 61 us, 4.5 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
 // rounded to bf16, in 32.  V, which is not turned, takes 32 bits with the same codes.  One row to a workgroup / two / four: 89 / 79 / 83 us for the append and the reading of it.
 // q, k and v are read and q is written past the caches: 8 prompts of 1024 tokens whose q, k and v a kernel before wrote 40.6 -> 28.6 us, with the xattn_prefill behind it 39.1 -> 32 (of
 // which it took its part); 64 of 256 81 -> 70, 256 of 16, 40 / 8 heads, 25 -> 21; steps of few tokens level.  A step's kernel takes 5 us, and the host's call binds it.

@@ -232,6 +232,18 @@ def test_read_batches(batch):
         assert (out[which][int(starts[-1]):] == 7).all()
 
 
+@pytest.mark.parametrize("heads,lens", [(8, [2040]), (8, [2041]), (8, [1500, 0, 9, 3001, 70]), (1, [16375, 1]), (1, [16376, 1]), (5, [3268, 1, 1])], ids=str)
+def test_read_of_eight_megabytes_and_around(heads, lens):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(sum(lens))
+    ranges = mx_util.Ranges(lens, heads, rows=[[torch.randn((n, heads, D), generator=g, device="cuda") for n in lens] for _ in range(2)])
+    starts, out = read(ranges, lens, lens, heads, extra=7)
+    for which in range(2):
+        for b, n in enumerate(lens):
+            assert torch.equal(out[which][int(starts[b]):int(starts[b + 1])].double(), ranges.values(which, b)[:n]), (which, b)
+        assert (out[which][int(starts[-1]):] == 7).all()
+
+
 def test_what_was_appended_is_read():
     """A prompt in two chunks and a single token, through both operators; the rows are those that the definition stores."""
     chunks = [70, 130, 1]
