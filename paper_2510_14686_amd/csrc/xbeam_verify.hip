@@ -328,9 +328,9 @@ __device__ __forceinline__ void weights(const float (&x)[8], double c, double to
 // P - r0 Q further from 0 than |r - r0| Q stays on its side, and the sum over those above is, exactly,
 //     A - (r - r0) B      A = sum (P - r0 Q), B = sum Q      over tokens with P > r0 Q
 // The others change it by |r - r0| Q each at most: the fifth sum is of Q over all within kNear r0 Q, and where that leaves more than kMayMiss of the sum open, or
-// r is further off than kNear, pick sums anew with r, alone.  That happens where p and q are nearly the same, and, logits of 16 bits lying on a grid,
-// where one of its steps meets r: about one row in 4000 (bf16) or 500 (fp16), and costs 60 us at 131072 logits.  (A pass of its own with r: verify_batch 64.7 -> 57.9 us,
-// verify_one 20.6 -> 17.9.)
+// r is further off than kNear, pick sums anew with r, alone.  That happens where p and q are nearly the same, and now and then where one of the steps of the grid
+// that logits of 16 bits lie on meets r (within kNear in one row of 4000 in bf16, of 500 in fp16, which mostly still leaves less open than that).  It costs 60 us
+// at 131072 logits.  (A pass of its own with r, always: 64 sequences of nine rows 64.7 us in place of 56.5, one of them 20.6 in place of 17.9.)
 constexpr double kNear = 0x1p-20, kMayMiss = 0x1p-30;
 
 // grid.x = parts, grid.y = sequences.
