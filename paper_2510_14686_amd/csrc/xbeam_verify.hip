@@ -422,17 +422,18 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams 
         all_left = lane_d(upto_left, 63);
     }
     // p nowhere above q: nothing could have fallen but by rounding
-    const bool rest = drafted && all_left > 0.0;
-    const double all = rest ? all_left : all_p, upto = rest ? upto_left : upto_p, mine = rest ? left : sums[0];
-    if (d.row < 0 || !(all > 0.0) || !(all < __builtin_inf())) {
+    bool rest = drafted && all_left > 0.0;
+    const double all = rest ? all_left : all_p;
+    double upto = rest ? upto_left : upto_p, mine = rest ? left : sums[0];
+    auto none = [&] {
         if (tid == 0) {
             // without a token that has all of p, it comes back: rounding alone let it fall
             const bool back = d.row >= 0 && d.mode == kWithout;
             prm.tokens[out] = back ? d.without : -1;
             if (prm.token_lp) prm.token_lp[out] = back ? 0.0f : __builtin_nanf("");
         }
-        return;
-    }
+    };
+    if (d.row < 0 || !(all > 0.0) || !(all < __builtin_inf())) return none();
     auto finish = [&](int token, double logit) {
         prm.tokens[out] = token;
         if (prm.token_lp) {
@@ -442,62 +443,76 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams 
             prm.token_lp[out] = (float)((logit * s.c - d.top - log2_d(z)) / kLog2e);
         }
     };
-    const double goal = u * all;
-    const unsigned long long hit = __ballot(lane < cut.parts && upto > goal), some = __ballot(mine > 0.0);
-    const int part = uniform(hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(some));
-    double before = lane_d(upto - mine, part);
-    const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
-    for (int step = first; step < end; step += kVerifyStep) {
-        const int i = step + kPickLogits * tid;
-        float x[kPickLogits], y[kPickLogits];
-        double w[kPickLogits];
+    double goal = u * all;
+    // A - (r - r0) B may leave something by rounding in a part whose tokens all have P <= r Q: 1e-28 of the sum, which a random number of 0 falls into.  Then it
+    // is the next part with a weight, or where none is left the last one before it.
+    while (last < 0) {
+        unsigned long long some = __ballot(mine > 0.0);
+        if (some == 0 && rest) {      // rounding in all parts
+            rest = false;
+            mine = sums[0];
+            upto = upto_p;
+            goal = u * all_p;
+            some = __ballot(mine > 0.0);
+        }
+        if (some == 0) return none();
+        const unsigned long long hit = some & __ballot(upto > goal);
+        const int part = uniform(hit ? __builtin_ctzll(hit) : 63 - __builtin_clzll(some));
+        double before = lane_d(upto - mine, part);
+        mine = lane == part ? 0.0 : mine;
+        const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
+        for (int step = first; step < end; step += kVerifyStep) {
+            const int i = step + kPickLogits * tid;
+            float x[kPickLogits], y[kPickLogits];
+            double w[kPickLogits];
 #pragma unroll
-        for (int j = 0; j < kPickLogits; ++j) {
-            x[j] = i + j < end ? to_float(s.p[i + j]) : kNegInf;
-            y[j] = rest && i + j < end ? to_float(s.q[i + j]) : kNegInf;
-        }
-        double sum = 0.0;
-        int top = -1;
+            for (int j = 0; j < kPickLogits; ++j) {
+                x[j] = i + j < end ? to_float(s.p[i + j]) : kNegInf;
+                y[j] = rest && i + j < end ? to_float(s.q[i + j]) : kNegInf;
+            }
+            double sum = 0.0;
+            int top = -1;
 #pragma unroll
-        for (int j = 0; j < kPickLogits; ++j) {
-            w[j] = i + j == d.without ? 0.0 : exp2_d(__builtin_fma((double)x[j], s.c, -d.top));
-            if (rest) w[j] = fmax(__builtin_fma(-ratio, exp2_d(__builtin_fma((double)y[j], s.dc, -d.draft_top)), w[j]), 0.0);
-            sum += w[j];
-            top = w[j] > 0.0 ? i + j : top;
-        }
-        const double scan = wave_scan_d(sum);
-        const unsigned long long with = __ballot(top >= 0);
-        top = with ? __builtin_amdgcn_readlane(top, 63 - __builtin_clzll(with | 1)) : -1;
-        __syncthreads();      // the step before has been read
-        if (lane == 63) {
-            totals[wave] = scan;
-            tops[wave] = top;
-        }
-        __syncthreads();
-        double at = before + (scan - sum);
-        for (int q = 0; q < kPickWaves; ++q) {
-            at += q < wave ? totals[q] : 0.0;
-            before += totals[q];
-            last = tops[q] > last ? tops[q] : last;
-        }
-        int here = kNone;
-        float logit = 0.0f;
+            for (int j = 0; j < kPickLogits; ++j) {
+                w[j] = i + j == d.without ? 0.0 : exp2_d(__builtin_fma((double)x[j], s.c, -d.top));
+                if (rest) w[j] = fmax(__builtin_fma(-ratio, exp2_d(__builtin_fma((double)y[j], s.dc, -d.draft_top)), w[j]), 0.0);
+                sum += w[j];
+                top = w[j] > 0.0 ? i + j : top;
+            }
+            const double scan = wave_scan_d(sum);
+            const unsigned long long with = __ballot(top >= 0);
+            top = with ? __builtin_amdgcn_readlane(top, 63 - __builtin_clzll(with | 1)) : -1;
+            __syncthreads();      // the step before has been read
+            if (lane == 63) {
+                totals[wave] = scan;
+                tops[wave] = top;
+            }
+            __syncthreads();
+            double at = before + (scan - sum);
+            for (int q = 0; q < kPickWaves; ++q) {
+                at += q < wave ? totals[q] : 0.0;
+                before += totals[q];
+                last = tops[q] > last ? tops[q] : last;
+            }
+            int here = kNone;
+            float logit = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kPickLogits; ++j) {
-            at += w[j];
-            const bool is = at > goal && w[j] > 0.0 && here == kNone;
-            logit = is ? x[j] : logit;
-            here = is ? i + j : here;
+            for (int j = 0; j < kPickLogits; ++j) {
+                at += w[j];
+                const bool is = at > goal && w[j] > 0.0 && here == kNone;
+                logit = is ? x[j] : logit;
+                here = is ? i + j : here;
+            }
+            const unsigned long long beyond = __ballot(here != kNone);
+            const int first_here = __builtin_amdgcn_readlane(here, beyond ? __builtin_ctzll(beyond) : 0);
+            if (lane == 0) heres[wave] = first_here;
+            __syncthreads();
+            int found = kNone;
+            for (int q = 0; q < kPickWaves; ++q) found = heres[q] < found ? heres[q] : found;
+            if (found == kNone) continue;
+            if (here == found) finish(here, (double)logit);
+            return;
         }
-        const unsigned long long beyond = __ballot(here != kNone);
-        const int first_here = __builtin_amdgcn_readlane(here, beyond ? __builtin_ctzll(beyond) : 0);
-        if (lane == 0) heres[wave] = first_here;
-        __syncthreads();
-        int found = kNone;
-        for (int q = 0; q < kPickWaves; ++q) found = heres[q] < found ? heres[q] : found;
-        if (found == kNone) continue;
-        if (here == found) finish(here, (double)logit);
-        return;
     }
     if (tid == 0) finish(last, (double)to_float(s.p[last]));      // the part's last one, where rounding leaves the goal just behind it
 }

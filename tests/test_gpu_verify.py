@@ -394,3 +394,29 @@ def test_a_workspace_of_the_callers():
     finally:
         torch.cuda.synchronize()
         xa.xattn_set_workspace(None, 0)
+
+
+def test_a_first_part_with_no_weight_and_a_number_of_zero():
+    """The first 2048 of 6144 tokens have the same logits in both rows, e^-40 of the others', and the draft row has the target's others in another order: p's sum is
+    q's, and the weights begin behind the first 2048.  The weights' sum may be off by 2^-30 of it, so a token up to there may come."""
+    c = Case(512, 2, 6144, "fp32", seed=19, sd=1.0)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(19)
+    c.target.normal_(0.0, 1.0, generator=g)
+    c.target[..., :2048] -= 40.0
+    c.draft.copy_(c.target[:, :1])
+    c.draft[..., 2048:] = torch.gather(c.draft[..., 2048:], 2, torch.rand((512, 1, 4096), generator=g, device="cuda").argsort(-1))
+    c.draft_tokens.fill_(-1)
+    c.uniforms.zero_()
+    c.call()
+    torch.cuda.synchronize()
+    assert c.accepted.tolist() == [0] * 512
+    target, draft = (x[:, 0].cpu().numpy().astype(np.longdouble) for x in (c.target, c.draft))
+    tokens, lps = c.tokens[:, 0].tolist(), c.lp[:, 0].tolist()
+    for b in range(512):
+        p, q = (np.exp(x[b] - x[b].max()) for x in (target, draft))
+        p, q = p / p.sum(), q / q.sum()
+        sums = np.cumsum(np.maximum(p - q, 0))
+        last = int(np.argmax(sums > 2.0 ** -30 * sums[-1]))
+        assert 0 <= tokens[b] <= last and last >= 2048, (b, tokens[b], last)
+        assert abs(lps[b] - float(np.log(p[tokens[b]]))) <= 2.0 ** -20 + 2.0 ** -23 * 60, b
