@@ -95,7 +95,7 @@ size_t xbeam_logprobs_workspace_bytes(int rows, int vocab, int top_k);
  * n_accepted   DEVICE int32 [batch]: drafts that stand; a sequence keeps kv_len - (q_len - 1 - n_accepted) rows of its cache
  * token_lp     DEVICE fp32 [batch, q_len] or NULL: ln p of every token given, 0 behind them
  * Outputs do not overlap the inputs or each other.
- * Logits of -inf are forbidden tokens.  A target row with +inf or NaN, or of nothing but -inf, has no probabilities: its draft falls, and the new
+ * Logits of -inf are forbidden tokens, and finite ones may have any size.  A target row with +inf or NaN, or of nothing but -inf, has no probabilities: its draft falls, and the new
  * token is -1 (token_lp NaN).  At a draft row without probabilities the draft falls and w = p.  Where rounding alone let a draft fall, p being
  * nowhere above q, w = p.
  * Numerics: whether a draft stands is decided with sums in 32 bits: p and q are off by 2^-20 of them at most, and 2^-25 for every power of two

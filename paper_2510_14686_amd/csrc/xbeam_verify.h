@@ -26,7 +26,7 @@ struct VerifyParams {
     int32_t* accepted;               // [batch]
     float* token_lp;                 // [batch, q_len] or null
     // workspace
-    float2* stats;                   // [rows, parts]: reference, sum (greedy: and the best token's key)
+    float2* stats;                   // [rows, parts]: largest logit, sum of exponentials over it
     uint64_t* best;                  // [target rows, parts], greedy
     double* sums;                    // [kVerifySums, batch, cut.parts]: see verify_weigh_kernel
     void* decisions;                 // [batch]

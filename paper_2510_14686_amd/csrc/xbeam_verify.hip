@@ -32,7 +32,8 @@ constexpr int kWaves = kVerifyThreads / 64;
 
 // What the first pass says about a sequence.
 struct Decision {
-    double top, draft_top;           // references of p's and q's exponents: the rows' maxima times scale * log2 e
+    double factor, draft_factor;     // of p's and q's exponents, in log2 units
+    double top, draft_top;           // their references: the rows' largest logits times the factor
     double ratio;                    // with kRest: of the sums of p's and q's weights, from 32 bits
     int row;                         // token t that the new one is drawn at, or -1: no probabilities there
     int accepted;
@@ -115,8 +116,18 @@ __device__ __forceinline__ uint64_t token_key(float x, int index) {
     return (uint64_t)(x == x ? k : 0u) << 32 | (uint32_t)~index;
 }
 
-// What a logit's exponent is, in log2 units: the same rounded factor wherever the first pass' sums are used.
+// The exponent of a logit x, in log2 units and over that of its row's largest one m, is (x - m) times this: the same rounded factor wherever the first pass'
+// sums are used.
 __device__ __forceinline__ float exponent_scale(float scale) { return (float)((double)scale * kLog2e); }
+
+// A sum's exponents are x c - r with one rounding, r = m c as rounded.  What that cut off is half of r's last digit and shared by all weights of the sum: 2^6 in 32 bits
+// where m c is 2^30, 2^-17 in 64 where it is 2^36.  Further from 0 this is a lesser c with which m c is just that: logits next to m in their type are
+// 2^6 and 2^12 powers of two below it with that one too, and weigh nothing among 2^24 tokens.
+template <typename F>
+__device__ __forceinline__ F factor_at(F c, F m, F most) {
+    if (__builtin_expect(__ballot(fabs(m) * c > most) != 0, 0) && fabs(m) * c > most) c = most / fabs(m);
+    return c;
+}
 
 __device__ __forceinline__ int drafts_of(const VerifyParams& prm, int b) {
     const int n = prm.n_drafts ? prm.n_drafts[b] : prm.q_len - 1;
@@ -139,7 +150,7 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
     const T* const p = static_cast<const T*>(is_draft ? prm.draft : prm.target) + (int64_t)r * (is_draft ? prm.draft_stride : prm.target_stride);
     const float c = exponent_scale(is_draft ? prm.draft_scale : prm.scale);
     const int first = part * cut.size, end = first + cut.size < prm.vocab ? first + cut.size : prm.vocab;
-    float m = kNegInf, ref = 0.0f, sum = 0.0f;
+    float m = kNegInf, f = c, ref = 0.0f, cut_off = 0.0f, sum = 0.0f;      // sum of 2^(x f - ref), ref + cut_off = m f
     uint64_t best = 0;
     // Four steps' loads go out together, and the running reference is looked at once for them.
     auto steps = [&](auto count, int i) {
@@ -153,16 +164,18 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
 #pragma unroll
             for (int j = 0; j < 8; ++j) top = fmaxf(top, x[k][j]);
         if (top > m) {
-            const float to = top * c;
-            sum *= fast_exp2(m == kNegInf ? 0.0f : ref - to);
+            f = factor_at(c, top, 0x1p30f);
+            ref = top * f;
+            const float off = __builtin_fmaf(top, f, -ref);
+            sum *= fast_exp2(m == kNegInf ? 0.0f : (m - top) * c + (off - cut_off));
             m = top;
-            ref = to;
+            cut_off = off;
         }
 #pragma unroll
         for (int k = 0; k < kCount; ++k)
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                sum += fast_exp2(__builtin_fmaf(x[k][j], c, -ref));
+                sum += fast_exp2(__builtin_fmaf(x[k][j], f, -ref));
                 if constexpr (kGreedy) {
                     const int at = i + k * kVerifyStep + j;
                     const uint64_t key = at < end ? token_key(x[k][j], at) : 0;
@@ -173,11 +186,11 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
     int i = first + 8 * tid;
     for (; i + 3 * kVerifyStep < end; i += 4 * kVerifyStep) steps(std::integral_constant<int, 4>(), i);
     for (; i < end; i += kVerifyStep) steps(std::integral_constant<int, 1>(), i);
-    __shared__ float refs[kWaves], sums[kWaves];
+    __shared__ float tops[kWaves], sums[kWaves];
     __shared__ uint64_t keys[kWaves];
-    const float mine = m == kNegInf ? kNegInf : ref, top = wave_max(mine);
+    const float top = wave_max(m);
     // a lane of nothing but -inf has 0, one with a NaN NaN
-    const float s = wave_sum(sum * (mine == kNegInf ? (sum == sum ? 0.0f : sum) : fast_exp2(mine - top)));
+    const float s = wave_sum(sum * (m == kNegInf ? (sum == sum ? 0.0f : sum) : fast_exp2((m - top) * c - cut_off)));
     if constexpr (kGreedy) {
 #pragma unroll
         for (int d = 1; d < 64; d *= 2) {
@@ -187,16 +200,16 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
         if (lane == 0) keys[wave] = best;
     }
     if (lane == 0) {
-        refs[wave] = top;
+        tops[wave] = top;
         sums[wave] = s;
     }
     __syncthreads();
     if (tid > 0) return;
-    float all = refs[0];
-    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, refs[w]);
+    float all = tops[0];
+    for (int w = 1; w < kWaves; ++w) all = fmaxf(all, tops[w]);
     float total = 0.0f;
     for (int w = 0; w < kWaves; ++w) {
-        total += refs[w] == kNegInf ? sums[w] : sums[w] * fast_exp2(refs[w] - all);
+        total += tops[w] == kNegInf ? sums[w] : sums[w] * fast_exp2((tops[w] - all) * c);
         if constexpr (kGreedy) best = keys[w] > best ? keys[w] : best;
     }
     prm.stats[(int64_t)row * cut.parts + part] = make_float2(all, total);
@@ -204,14 +217,14 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_read_kernel(VerifyParam
 }
 
 // ---------------------------------------------------------------------------------- decide
-// A row's largest exponent (as the first pass rounded it) and log2 of its sum; NaN where it has no probabilities.  By one wave.
+// A row's largest logit and log2 of its sum, which counts that as 1; no finite number where it has no probabilities.  By one wave.
 struct RowSum {
     double log2_sum, top;
 };
-__device__ __forceinline__ RowSum row_sum(float2 mine) {
+__device__ __forceinline__ RowSum row_sum(float2 mine, double c) {
     const float top = wave_max(mine.x);
-    const double s = wave_sum_d(mine.x == kNegInf ? (double)mine.y : (double)mine.y * exp2_d((double)mine.x - (double)top));
-    return RowSum{log2_d(s) + (double)top, (double)top};
+    const double s = wave_sum_d(mine.x == kNegInf ? (double)mine.y : (double)mine.y * exp2_d(((double)mine.x - (double)top) * c));
+    return RowSum{log2_d(s), (double)top};
 }
 template <typename T>
 __device__ __forceinline__ double logit_at(const void* rows, int64_t stride, int64_t row, int token) { return (double)to_float(static_cast<const T*>(rows)[row * stride + token]); }
@@ -238,8 +251,8 @@ __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(Verify
         const bool is_token = x >= 0 && x < prm.vocab;
         const double at = is_token ? logit_at<T>(prm.target, prm.target_stride, row, x) : 0.0;
         const double draft_at = is_token && with_draft ? logit_at<T>(prm.draft, prm.draft_stride, draft_row, x) : 0.0;
-        const RowSum p = row_sum(mine);
-        const double lp = at * c - p.log2_sum;
+        const RowSum p = row_sum(mine, c);
+        const double lp = (at - p.top) * c - p.log2_sum;
         double draft_top = 0.0, ratio = 0.0;
         int best = -1;
         bool fine = false;
@@ -255,10 +268,10 @@ __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(Verify
         } else if (judges) {
             double lq = 0.0;
             if (prm.draft) {
-                const RowSum q = row_sum(drafts);
+                const RowSum q = row_sum(drafts, dc);
                 draft_top = q.log2_sum - q.log2_sum == 0.0 ? q.top : __builtin_nan("");
-                lq = draft_at * dc - q.log2_sum;
-                ratio = exp2_d((p.log2_sum - p.top) - (q.log2_sum - q.top));
+                lq = (draft_at - q.top) * dc - q.log2_sum;
+                ratio = exp2_d(p.log2_sum - q.log2_sum);
             }
             // u q < p, where the row has probabilities: NaN and infinities are neither
             fine = is_token && draft_top == draft_top && (double)prm.uniforms[row] * exp2_d(lq) < (lp == lp ? exp2_d(lp) : 0.0);
@@ -278,8 +291,10 @@ __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(Verify
     d.accepted = 0;
     while (d.accepted < n && stands[d.accepted]) ++d.accepted;
     const int at = d.accepted;
-    d.top = tops[at];
-    d.draft_top = draft_tops[at];
+    d.factor = factor_at((double)prm.scale * kLog2e, tops[at], 0x1p36);
+    d.draft_factor = factor_at((double)prm.draft_scale * kLog2e, draft_tops[at], 0x1p36);
+    d.top = tops[at] * d.factor;
+    d.draft_top = draft_tops[at] * d.draft_factor;
     d.ratio = ratios[at];
     d.row = lses[at] - lses[at] == 0.0 ? at : -1;
     d.mode = kGreedy || at == n || !(d.draft_top == d.draft_top) ? kPlain : prm.draft ? kRest : kWithout;
@@ -289,7 +304,7 @@ __global__ __launch_bounds__(64 * kDecideWaves) void verify_decide_kernel(Verify
         float lp = tid < at ? (float)(lps[tid] / kLog2e) : 0.0f;
         if (kGreedy && tid == at) {
             token = d.row >= 0 ? tokens[at] : -1;
-            lp = d.row >= 0 ? (float)((logit_at<T>(prm.target, prm.target_stride, (int64_t)b * prm.q_len + at, token) * c - lses[at]) / kLog2e) : __builtin_nanf("");
+            lp = d.row >= 0 ? (float)(((logit_at<T>(prm.target, prm.target_stride, (int64_t)b * prm.q_len + at, token) - tops[at]) * c - lses[at]) / kLog2e) : __builtin_nanf("");
         }
         prm.tokens[(int64_t)b * prm.q_len + tid] = token;
         if (prm.token_lp) prm.token_lp[(int64_t)b * prm.q_len + tid] = lp;
@@ -313,8 +328,8 @@ __device__ __forceinline__ Source<T> source_of(const VerifyParams& prm, int b, c
     Source<T> s;
     s.p = static_cast<const T*>(prm.target) + ((int64_t)b * prm.q_len + d.row) * prm.target_stride;
     s.q = d.mode == kRest ? static_cast<const T*>(prm.draft) + ((int64_t)b * (prm.q_len - 1) + d.row) * prm.draft_stride : nullptr;
-    s.c = (double)prm.scale * kLog2e;
-    s.dc = (double)prm.draft_scale * kLog2e;
+    s.c = d.factor;
+    s.dc = d.draft_factor;
     return s;
 }
 // Unnormalised weights of eight tokens.
@@ -439,8 +454,8 @@ __global__ __launch_bounds__(kPickThreads) void verify_pick_kernel(VerifyParams 
         if (prm.token_lp) {
             double z = all_p;      // without the token left out
             const double less = d.without < 0 ? (double)kNegInf : (double)to_float(s.p[d.without]);
-            if (less > kNegInf) z += exp2_d(less * s.c - d.top);
-            prm.token_lp[out] = (float)((logit * s.c - d.top - log2_d(z)) / kLog2e);
+            if (less > kNegInf) z += exp2_d(__builtin_fma(less, s.c, -d.top));
+            prm.token_lp[out] = (float)((__builtin_fma(logit, s.c, -d.top) - log2_d(z)) / kLog2e);
         }
     };
     double goal = u * all;

@@ -420,3 +420,46 @@ def test_a_first_part_with_no_weight_and_a_number_of_zero():
         last = int(np.argmax(sums > 2.0 ** -30 * sums[-1]))
         assert 0 <= tokens[b] <= last and last >= 2048, (b, tokens[b], last)
         assert abs(lps[b] - float(np.log(p[tokens[b]]))) <= 2.0 ** -20 + 2.0 ** -23 * 60, b
+
+
+@pytest.mark.parametrize("far", [5e10, -5e10, 1e11, -1e11, -1e30, 3e38, -3.4028234663852886e38])
+@pytest.mark.parametrize("drafts", ["logits", "certain", "greedy"])
+def test_finite_logits_of_any_size_have_probabilities(drafts, far):
+    """So far from 0 a row's logits are all one value, and those of its tokens that lie a step of fp32 above it share p."""
+    c = Case(24, 3, 3000, "fp32", "logits" if drafts == "greedy" else drafts, seed=20, greedy=drafts == "greedy")
+    c.target.fill_(far)
+    c.target[8:, :, 100:103] = float(np.nextafter(np.float32(far), np.float32(0)))
+    c.target[16:, :, 2900:] = -math.inf
+    c.target[16:20, :, 7] = 1.0                # has p alone where far is below it, none of it where above
+    c.draft_tokens[:, 1] = 101
+    if c.draft is not None:
+        c.draft[:12] = -far
+        c.draft[:6, :, 102] = float(np.nextafter(np.float32(-far), np.float32(0)))
+    c.call()
+    c.check()
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 20, 1.0, 2.0 ** -20])
+@pytest.mark.parametrize("dtype,big", [("fp16", 64000.0), ("fp16", -65504.0), ("bf16", 3e38), ("bf16", -3e38), ("fp32", 1e34)])
+def test_scales_and_logits_at_their_ends(dtype, big, scale):
+    for drafts in ("logits", "certain"):
+        c = Case(16, 3, 2500, dtype, drafts, seed=21, scale=scale, draft_scale=1.0)
+        c.target[:8] = big
+        c.target[8:, :, ::5] = big
+        c.draft_tokens[:, 0] = 5
+        c.call()
+        c.check()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+def test_tokens_forbidden_by_the_lowest_value(dtype):
+    for drafts in ("logits", "certain"):
+        c = Case(24, 4, 5000, dtype, drafts, seed=22)
+        low = torch.finfo(c.target.dtype).min
+        c.target[:, :, ::3] = low
+        if c.draft is not None:
+            c.draft[:12, :, ::3] = low
+            c.draft[12:, :, 1::3] = low
+        c.target[20:] = low                    # nothing else: all tokens are as likely
+        c.call()
+        c.check()
