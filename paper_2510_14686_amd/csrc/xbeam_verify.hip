@@ -339,7 +339,8 @@ __device__ __forceinline__ void weights(const float (&x)[8], double c, double to
 }
 
 // With P and Q for the weights of p and q as they come and r for the ratio of their sums, max(0, p - q) is max(0, P - r Q) but for a factor.  Its sum
-// needs r first, yet the row is read once: the first pass says r0, off by 2^-21.6 of r at most in 1400 rows of 5000 to 131072 logits.  A token with
+// needs r first, yet the row is read once: the first pass says r0, off by 2^-21 of r at most in 600 pairs of rows of 5000 to 131072 logits, up to 100 from 0, with
+// scales of their own from 1/4 to 4 (its sums are relative to the largest logit itself, so how far that lies from 0 and which factor it has do not count).  A token with
 // P - r0 Q further from 0 than |r - r0| Q stays on its side, and the sum over those above is, exactly,
 //     A - (r - r0) B      A = sum (P - r0 Q), B = sum Q      over tokens with P > r0 Q
 // The others change it by |r - r0| Q each at most: the fifth sum is of Q over all within kNear r0 Q, and where that leaves more than kMayMiss of the sum open, or

@@ -463,3 +463,29 @@ def test_tokens_forbidden_by_the_lowest_value(dtype):
         c.target[20:] = low                    # nothing else: all tokens are as likely
         c.call()
         c.check()
+
+
+def test_no_row_takes_the_long_way_for_where_its_logits_lie():
+    """Rows of logits moved by a constant, with temperatures of their own, take as long as others: the ratio of the sums of p and q that the first pass gives does not
+    depend on that.  (A row whose sums are made anew takes 60 us more, four times a call's time.  Least of several runs, all calls in turn.)"""
+    cases = [Case(4, 2, 131072, "fp32", seed=23)]
+    for scale, draft_scale, far in ((0.5, 0.5, 300.0), (1.3, 0.6, 100.0), (1 / 0.65, 1 / 0.65, 100.0), (0.2, 1.0, 1000.0)):
+        cases.append(Case(4, 2, 131072, "fp32", seed=23, scale=scale, draft_scale=draft_scale))
+        cases[-1].target += far
+    least = [math.inf] * len(cases)
+    for c in cases:
+        c.draft_tokens.fill_(-1)
+        c.call()
+    for _ in range(8):
+        for i, c in enumerate(cases):
+            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+            torch.cuda.synchronize()
+            begin.record()
+            for _ in range(20):
+                c.call()
+            end.record()
+            torch.cuda.synchronize()
+            least[i] = min(least[i], begin.elapsed_time(end) / 20)
+    assert max(least[1:]) < 2 * least[0], least
+    for c in cases:
+        c.check()
