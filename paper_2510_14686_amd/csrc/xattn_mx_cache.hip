@@ -283,13 +283,11 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
 
 // A wave takes four rows, 16 lanes a row, of four heads (grid.y): a row's sequence is looked for once for them, and rows that follow each other share
 // the lines of the cache.  (All heads in a workgroup: 500 rows of 40 heads 7.2 -> 10.6 us, large calls level.)  Bound by HBM: 28672 rows of 8
-// heads 24.5 us, 6.1 TB/s.
-// Results of 8 MiB and more go past the caches (kPast).  Written through them, they push out lines that others then have to write: that call 33.7 us, and 48 where a kernel before it
-// left the caches full, 32 so.  A following xattn_prefill of 128 tokens, which finds less there, takes most of that back: both 114 us and 115; 36.0 and 34.5 with 4096
-// rows, 206 and 211 with 65536, 20.0 and 21.4 with 512, which stay in the caches.
-constexpr int64_t kReadPast = (8 << 20) / (4 * kHeadDim);      // rows of heads, K's and V's
+// heads 33.4 us, 4.5 TB/s, 26.4 where the results lie in the caches already.
+// Results stay in the caches for what reads them next.  Past them this call alone would be shorter, 24.1 us, but not with an xattn_prefill behind it: 28672 rows and 128 tokens
+// 102.6 -> 104.4, four of 4096 and 64 57.4 -> 59.0, and where a kernel in front has filled the caches 109.6 -> 114 and 60.5 -> 70.5.  (Better so are 16 tokens behind 28672 rows, 65.1 ->
+// 62.2, and 16384 rows of 40 heads for as many query heads, 177 -> 167; behind writes 75.2 -> 74.5 and 199 -> 209.)
 constexpr int kReadRows = 16, kReadHeads = 4;
-template <bool kPast>
 __global__ __launch_bounds__(256) void read_mx_kernel(ReadMxParams prm) {
     const int lane = threadIdx.x & 63, wave = uniform((int)(threadIdx.x >> 6)), m = lane & 15;
     const int row0 = blockIdx.x * kReadRows + 4 * wave;
@@ -341,13 +339,8 @@ __global__ __launch_bounds__(256) void read_mx_kernel(ReadMxParams prm) {
         if (head0 + h >= prm.n_kv_heads) break;
         uint16_t* const k = prm.k_out + to + (head0 + h) * kHeadDim;
         uint16_t* const v = prm.v_out + to + (head0 + h) * kHeadDim;
-        if constexpr (kPast) {
-            store_past(unpack(kc[h], ks[h]), k);
-            store_past(unpack(vc[h], vs[h]), v);
-        } else {
-            *reinterpret_cast<u32x4_t*>(k) = unpack(kc[h], ks[h]);
-            *reinterpret_cast<u32x4_t*>(v) = unpack(vc[h], vs[h]);
-        }
+        *reinterpret_cast<u32x4_t*>(k) = unpack(kc[h], ks[h]);
+        *reinterpret_cast<u32x4_t*>(v) = unpack(vc[h], vs[h]);
     }
 }
 
@@ -375,8 +368,7 @@ hipError_t launch_rope_mx(const RopeParams& prm, hipStream_t stream) {
 
 hipError_t launch_read_mx(const ReadMxParams& prm, hipStream_t stream) {
     const int rows = (prm.total_q + kReadRows - 1) / kReadRows, heads = (prm.n_kv_heads + kReadHeads - 1) / kReadHeads;
-    const dim3 grid((unsigned)rows, (unsigned)heads);
-    return (int64_t)prm.total_q * prm.n_kv_heads >= kReadPast ? launch(read_mx_kernel<true>, grid, 256, stream, prm) : launch(read_mx_kernel<false>, grid, 256, stream, prm);
+    return launch(read_mx_kernel, dim3((unsigned)rows, (unsigned)heads), 256, stream, prm);
 }
 
 }  // namespace xattn
