@@ -6,8 +6,10 @@
 // A prompt's append is bound by HBM and, beside it, the arithmetic of codes: two prompts of 4096 to 8191 tokens, 32 / 8 heads, three axes, 273 MB in
 // 61 us, 4.5 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
 // rounded to bf16, in 32.  V, which is not turned, takes 32 bits with the same codes.  One row to a workgroup / two / four: 89 / 79 / 83 us for the append and the reading of it.
-// q, k and v are read and q is written past the caches: 8 prompts of 1024 tokens whose q, k and v a kernel before wrote 40.6 -> 28.6 us, with the xattn_prefill behind it 39.1 -> 32 (of
-// which it took its part); 64 of 256 81 -> 70, 256 of 16, 40 / 8 heads, 25 -> 21; steps of few tokens level.  A step's kernel takes 5 us, and the host's call binds it.
+// q, k and v are read past the caches, which keep the codes and the turned q for the calls behind: from the kernel that writes q, k and v to the end of xattn_prefill, by way of
+// xattn_read_kvcache_mx, 8 prompts of 1024 tokens, 32 / 8 heads, 178.8 us and 179.8 with plain loads, 64 of 256 282.9 and 298.2, two of 6000 655 and 663.  With q written past the caches, too, this
+// call alone is shorter (two of 6000 behind that kernel 54.5 -> 43), but what reads q is longer: 181.5, 284.3 and 662 together, of 64 / 8 heads one of 2048 114.4 -> 116.8 (256 of 16, 40 / 8 heads,
+// 189.6 -> 186.3); steps with xattn_decode_mx level.  A step's kernel takes 5 us, and the host's call binds it.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -106,9 +108,8 @@ __device__ __forceinline__ Encoded encode(u32x4_t x) {
     return Encoded{convert(f, __uint_as_float((uint32_t)(e + 127) << 23)), most < 0x7f80u ? e + 127 : kMxNanScale};
 }
 
-// Values that are read once, or that this kernel does not need again: past the caches, which keep what else is in them.
+// Values that are read once: past the caches, which keep what else is in them.
 __device__ __forceinline__ u32x4_t load_once(const uint16_t* p) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(p)); }
-__device__ __forceinline__ void store_past(u32x4_t x, uint16_t* p) { __builtin_nontemporal_store(x, reinterpret_cast<u32x4_t*>(p)); }
 
 __device__ __forceinline__ void widen(u32x4_t x, double (&d)[8]) {
 #pragma unroll
@@ -240,8 +241,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_mx_kernel(RopeParams prm) {
                 }
             }
         }
-        store_past(x, prm.q_out + it.at + it.at0);
-        store_past(y, prm.q_out + it.at + it.at1);
+        *reinterpret_cast<u32x4_t*>(prm.q_out + it.at + it.at0) = x;
+        *reinterpret_cast<u32x4_t*>(prm.q_out + it.at + it.at1) = y;
     }
 
     for (int item = tid; item < kv_all; item += kRopeThreads) {
