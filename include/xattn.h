@@ -391,7 +391,8 @@ int xattn_rope_kvcache(const void* q, const void* k_new, const void* v_new, int6
  * KV cache of 4 bits a value.  A head's row of 128 values is four blocks of 32, each with a scale 2^e (a byte, e + 127), and a value is one of 0,
  * 0.5, 1, 1.5, 2, 3, 4, 6 times that, with a sign (e2m1 elements and e8m0 scales of the OCP Microscaling Formats): 68 bytes a row instead of
  * 256.  e is the least from -125 to 126 with every value within 7 * 2^e; a value goes to the nearest code, of two as near to the even one.  A
- * block with a NaN or an infinity is stored as NaN (scale byte 255).
+ * block with a NaN or an infinity is stored as NaN (scale byte 255).  Codes 4 and 6 at e = 126, the nearest to values from 1.75 * 2^127 on, stand for 2^128 and
+ * more, which neither bf16 nor fp32 holds: to the operators below they are infinities.
  * Ranges hold tiles of XATTN_MX_TILE_TOKENS tokens: tile i of KV head h is at (i * n_kv_heads + h) * XATTN_MX_TILE_BYTES and has token t = 16 s + u of
  * it (0 <= u < 16), the lower half of a byte first:
  *     K  codes of values 32 c .. + 31 at 1024 s + 256 c + 16 u                 scale of block c at 4096 + 4 (16 c + u) + s
@@ -402,7 +403,7 @@ int xattn_rope_kvcache(const void* q, const void* k_new, const void* v_new, int6
  * xattn_mx_range_bytes   0 tokens: 0.  0 and a message for sizes that are not supported (1..1024 heads, head_dim 128).
  * xattn_rope_kvcache_mx  xattn_rope_kvcache, arguments and checks alike, but into such ranges: K is rotated in double and stored as codes from
  *                        there (no rounding in between), V as it is.  head_dim 128.  Rows are written whole, and nothing else is.
- * xattn_read_kvcache_mx  the packed rows of a batch as bf16, exactly what the codes stand for: row q_starts[b] + t of k_out and v_out
+ * xattn_read_kvcache_mx  the packed rows of a batch as bf16, exactly what the codes stand for (from 2^128 on infinity): row q_starts[b] + t of k_out and v_out
  *                        [total_q, n_kv_heads, 128] (16-byte aligned) is row kv_lens[b] - q_len + t of sequence b, with q_len = q_starts[b + 1] -
  *                        q_starts[b]; all rows where that is kv_lens[b].  Rows before the first are zeros; rows from q_starts[batch] on are left
  *                        as they were.  (A prompt's chunk behind a cached part: read all rows, attend them with xattn_prefill.)
@@ -410,7 +411,7 @@ int xattn_rope_kvcache(const void* q, const void* k_new, const void* v_new, int6
  * xattn_decode_mx        xattn_decode over such ranges: same arguments, shapes, masks, outputs, stream, capture and ownership rules, and the
  *                        same workspace, of at least xattn_decode_mx_workspace_bytes.  scale * log2 e finite, up to 1024 KV heads.  K and V enter the products
  *                        exactly; scores, maxima and sums are fp32; a softmax weight enters the value product as two bf16 (16 significant bits).
- *                        A NaN or an infinity in a sequence's rows or queries leaves its results unspecified, and no others.  XATTN_CFG_* do not apply.
+ *                        A NaN or an infinity in a sequence's rows (2^128 and more among them) or queries leaves its results unspecified, and no others.  XATTN_CFG_* do not apply.
  */
 #define XATTN_MX_TILE_TOKENS 64
 #define XATTN_MX_TILE_BYTES 4352

@@ -26,7 +26,7 @@ constexpr int kMxCodeBytes = 4096;
 constexpr int kMxTileBytes = kMxCodeBytes + 256;
 // A block's scale exponent: the least e with all values within 7 * 2^e, so that none is further from its code than half of the
 // widest step, 4 to 6.  (Root mean square error of N(0, 1) with 6 / 7 / 8 in 7's place: 0.1153 / 0.1118 / 0.1150.)  From -125 on the least
-// code, half of the scale, is a normal number of bf16 and fp32.
+// code, half of the scale, is a normal number of bf16 and fp32.  At 126 only codes up to 3 are: 4 and 6 are read as infinities.
 constexpr int kMxLeastExp = -125, kMxMostExp = 126;
 constexpr int kMxNanScale = 255;
 

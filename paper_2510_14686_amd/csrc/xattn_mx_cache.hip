@@ -1,7 +1,7 @@
 // Rows into and out of a cache of 4 bits a value (xattn_rope_kvcache_mx, xattn_read_kvcache_mx; the cache: xattn_mx.h).
 //
 //   append  (x, y) -> (x cos a - y sin a, y cos a + x sin a) as in xattn_rope.hip; q rounded to bf16, k and v to codes with a scale per 32 values
-//   read    code * scale, exact in bf16
+//   read    code * scale, exact in bf16 (infinity from 2^128 on)
 //
 // A prompt's append is bound by HBM and, beside it, the arithmetic of codes: two prompts of 4096 to 8191 tokens, 32 / 8 heads, three axes, 273 MB in
 // 61 us, 4.5 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is

@@ -289,3 +289,43 @@ def test_ranges_of_more_than_four_gigabytes():
         assert torch.equal(out[which].double(), mx_util.decode(*want))
         nonzero = int((caches[which].view(-1, heads * mx_util.TILE_BYTES).amax(1) > 0).sum())
         assert nonzero == len(set((row // 64).tolist()))
+
+
+def test_the_largest_scales():
+    """Scale bytes 252 and 253 with every code: 4 and 6 times 2^126 are past the largest bf16, all others exact."""
+    lens = [130, 64]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(10)
+    ranges = mx_util.Ranges(lens, 2, g=g)
+    for side in ranges.caches:
+        for c in side:
+            scale = c.view(-1, mx_util.TILE_BYTES)[:, mx_util.CODES:]
+            scale.copy_(252 + scale % 2)
+    starts, out = read(ranges, lens, lens, 2)
+    for which in range(2):
+        for b, n in enumerate(lens):
+            want = ranges.values(which, b)
+            assert int((want.abs() >= 2.0 ** 128).sum()) > 1000 and int((want.abs() == 1.5 * 2.0 ** 127).sum()) > 1000
+            assert torch.equal(out[which][int(starts[b]):int(starts[b + 1])].double(), torch.where(want.abs() < 2.0 ** 128, want, want.sign() * torch.inf))
+
+
+def test_the_largest_values_of_bf16():
+    """Appended and read: from 1.75 * 2^127 on a value comes back infinite, below it is off by a quarter of 2^127 at most, half a step of its code."""
+    b = Batch([(32, 32)], 2, 2, [0], seed=11)
+    edge = torch.tensor([1.734375 * 2.0 ** 127, 1.75 * 2.0 ** 127, 1.7578125 * 2.0 ** 127, 3.3895e38, 2.0 ** 127, 1.5 * 2.0 ** 127, 0.0, 1.0], device="cuda", dtype=torch.float64)
+    for x in (b.k_new, b.v_new):
+        v = x.unflatten(1, (2, 4, 32))
+        v[:4] = edge[:4].bfloat16()[:, None, None, None]
+        v[4:8] = edge[4:8].bfloat16()[:, None, None, None]
+        v[8:] = edge.bfloat16().repeat(4)
+        v[16:] *= -1
+    b.was = [x.clone() for x in (b.q, b.k_new, b.v_new)]
+    b.call()
+    b.check()
+    _, out = read(b.ranges, [32], [32], 2)
+    for which, x in enumerate((b.k_new, b.v_new)):
+        x, got = x.unflatten(1, (2, D)).double(), out[which].double()
+        beyond = x.abs().unflatten(-1, (4, 32)).amax(-1, keepdim=True) > 1.75 * 2.0 ** 127      # blocks of e = 126
+        infinite = (beyond & (x.abs().unflatten(-1, (4, 32)) >= 1.75 * 2.0 ** 127)).flatten(-2)
+        assert int(infinite.sum()) and torch.equal(got.isinf(), infinite) and torch.equal(got.sign()[infinite], x.sign()[infinite])
+        assert ((got - x).abs()[~infinite] <= 2.0 ** 127 / 4).all()
