@@ -6,7 +6,9 @@
 // run of tiles each; a sequence that the waves cut among themselves is put together in LDS, one that pieces cut by the merge kernel.
 //
 // Bound by HBM with many keys: 64 sequences of 512 to 4096, 32 / 8 heads, 35.2 us; 16 of 16384 to 32768, 64 / 8 heads, 76 us (5.9 TB/s); 128 of
-// 1028 to 8196, four tokens, 32 / 8 heads, 107 us (5.8 TB/s); with few by the dependent steps of two kernels, 9 to 10 us.  What the code owes to that:
+// 1028 to 8196, four tokens, 32 / 8 heads, 107 us (5.8 TB/s); with few by the dependent steps of two kernels, 9 to 10 us.  With 32 rows to a KV head by the issue of
+// conversions, softmax and products (187 MB in 54 us, 3.8 TB/s in the kernel; vector units 62 %, matrix pipes 35 %), with 64, whose two workgroups a piece each convert all codes,
+// twice per byte (100 MB in 54 us).  What the code owes to that:
 //  - Codes become bf16 by a conversion with the scale, exactly, two to an instruction, and enter bf16 matrix products.  The scaled products
 //    that take codes as they are would want q in 8 bits: in three parts of e4m3 their sums are off by 7e-5 of sum |q k|, these by 1e-7.
 //  - Codes lie as the products' lanes hold them, so every load is 16 bytes a lane of one run of 1 KiB and nothing passes through LDS.

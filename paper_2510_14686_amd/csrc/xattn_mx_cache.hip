@@ -4,8 +4,8 @@
 //   read    code * scale, exact in bf16 (infinity from 2^128 on)
 //
 // A prompt's append is bound by HBM and, beside it, the arithmetic of codes: two prompts of 4096 to 8191 tokens, 32 / 8 heads, three axes, 273 MB in
-// 61 us, 4.5 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
-// rounded to bf16, in 32.  V, which is not turned, takes 32 bits with the same codes.  One row to a workgroup / two / four: 89 / 79 / 83 us for the append and the reading of it.
+// 62 us, 4.4 TB/s.  K is rotated in 64 bits, since a value next to the border of two codes goes to one or the other by its last digit; q, which is
+// rounded to bf16, in 32.  V, which is not turned, takes 32 bits with the same codes.
 // q, k and v are read past the caches, which keep the codes and the turned q for the calls behind: from the kernel that writes q, k and v to the end of xattn_prefill, by way of
 // xattn_read_kvcache_mx, 8 prompts of 1024 tokens, 32 / 8 heads, 178.8 us and 179.8 with plain loads, 64 of 256 282.9 and 298.2, two of 6000 655 and 663.  With q written past the caches, too, this
 // call alone is shorter (two of 6000 behind that kernel 54.5 -> 43), but what reads q is longer: 181.5, 284.3 and 662 together, of 64 / 8 heads one of 2048 114.4 -> 116.8 (256 of 16, 40 / 8 heads,
@@ -346,8 +346,8 @@ __global__ __launch_bounds__(256) void read_mx_kernel(ReadMxParams prm) {
 }
 
 // Rows per workgroup.  Fewer rows, more workgroups whose waits pass at once; more rows, fewer threads without work.  Of 1 / 2 / 4 rows each, in us: 256 rows of 40 / 8 heads
-// 5.5 / 7.3 / 10.6, 1024 8.8 / 9.8 / 12.2, 2048 15.3 / 13.4 / 16.0, 8192 43.6 / 38.2 / 41.1; of 64 / 8 1024 10.8 / 11.6 / 14.7, 8192 63 / 60.6 / 64; of 8 / 2 1024
-// 5.6 / 5.8 / 5.4, 4096 12.7 / 10.1 / 8.5, 8192 22.8 / 18.0 / 15.2.
+// 6.4 / 8.3 / 11.6, 1024 9.7 / 11.5 / 14.2, 1536 16.0 / 14.0 / 17.6, 2048 19.4 / 16.8 / 19.4, 8192 58.3 / 51.0 / 50.2; of 64 / 8 1024 11.5 / 13.5 / 18.8, 8192 69.6 / 62.5 / 66.0; of
+// 8 / 2 1024 6.3 / 6.6 / 6.2, 1536 8.4 / 7.1 / 7.1, 4096 16.3 / 12.4 / 9.7, 8192 30.5 / 22.6 / 17.7.
 int rows_per_workgroup(const RopeParams& prm) {
     if (prm.total_q < 1536) return 1;
     return (prm.n_q_heads + 2 * prm.n_kv_heads) * (kHeadDim / 16) > kRopeThreads / 2 ? 2 : 4;
