@@ -12,8 +12,9 @@
 // 64 bits because the borders between 100000 tokens lie 10^-5 apart on average and closer where it matters: with sums in 32 bits one token in
 // a hundred would be another one's neighbour.  The row's probabilities are worked out anew in every pass: to keep them would be 8 bytes per logit.
 // 64 sequences of four drafts, 131072 logits in bf16, 151 MB: 57.4 us, of which read 30 (5 TB/s, HBM), decide 4.6, weigh 19.8 (the 64-bit exponentials, a wave's
-// instruction taking 8 cycles), pick 5.  Greedy, 84 MB: 32.3 us, of which read 27.5 (exponentials and keys, the vector units busy throughout).  With 64 bits in the first pass already and none but pick behind it 20 us more; one sequence alone, four kernels
-// of dependent steps, 18.  exp2_d needs its eight multiply-adds: rounding by a large constant instead of rndne, cvt and ldexp is slower.
+// instruction taking 8 cycles), pick 5.  With 64 bits in the first pass already and none but pick behind it 20 us more; one sequence alone, four kernels
+// of dependent steps, 17.  exp2_d needs its eight multiply-adds: rounding by a large constant instead of rndne, cvt and ldexp is slower.  Greedy, 84 MB:
+// 32.3 us, of which read 27.5 (exponentials and keys, the vector units busy throughout).
 #include <hip/hip_runtime.h>
 #include <hip/hip_fp16.h>
 #include <stdint.h>
